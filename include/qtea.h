@@ -42,7 +42,7 @@
 extern "C" {
 #endif
 
-#define QTEA_ABI_VERSION 9
+#define QTEA_ABI_VERSION 10
 #define QTEA_MAX_BATCH 16
 
 enum qtea_status {

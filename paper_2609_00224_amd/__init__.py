@@ -3,7 +3,9 @@
 The binding marshals arguments only: every step of the GEMV runs in the HIP
 kernels of ``csrc/qtea.hip``, ``csrc/grouped.hip``, ``csrc/grouped_mma.hip``,
 ``csrc/tern_mfma.hip`` and ``csrc/tern_solo.hip`` behind the C ABI of ``include/qtea.h``, and every step of the offline
-quantizer in those of ``csrc/quant.hip`` behind ``include/qtea_quant.h``.  Torch
+quantizer in those of ``csrc/quant.hip`` behind ``include/qtea_quant.h``.  The
+serving operators around the products (paged cache, attention, draft
+verification; ``include/qtea_serve.h``) are bound in ``serving.py``.  Torch
 is used to allocate device memory and to name the current HIP stream.
 There is no CPU fallback: if the library is not built, loading it raises.
 
@@ -12,13 +14,20 @@ qtea_packed_bytes_e4m3, qtea_pack_e4m3, qtea_packed_bytes_g128, qtea_pack_g128,
 qtea_workspace_bytes, qtea_workspace_init, qtea_gemv, qtea_gemm_lowbatch,
 qtea_debug_unpack, qtea_read_ceiling, qtea_status_string, qtea_abi_version,
 qtea_grouped_plan_bytes, qtea_grouped_plan, qtea_grouped_gemv, qtea_grouped_status,
-qtea_quant_hessian, qtea_quant_workspace_bytes, qtea_quantize.
+qtea_quant_hessian, qtea_quant_workspace_bytes, qtea_quantize, qtea_kv_append,
+qtea_kv_read, qtea_attention_workspace_bytes, qtea_paged_attention,
+qtea_verify_workspace_bytes, qtea_verify_draft.
 """
 from __future__ import annotations
 
 import ctypes
 import os
 from dataclasses import dataclass
+
+from . import serving
+from .serving import (KV_FORMATS, QTEA_BF16, QTEA_F16, QTEA_F32, QTEA_KV_BLOCK, KvCache, QteaKvBatch, QteaKvCache,  # noqa: F401
+                      new_attention_workspace, new_kv_cache, new_verify_workspace, qtea_attention_workspace_bytes,
+                      qtea_kv_append, qtea_kv_read, qtea_paged_attention, qtea_verify_draft, qtea_verify_workspace_bytes)
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libqtea.so")
@@ -38,7 +47,7 @@ QTEA_ERR_HIP = -6
 QTEA_ERR_NOT_POSITIVE = -7
 QTEA_QUANT_GROUP = 128
 QTEA_MAX_BATCH = 16
-QTEA_ABI_VERSION = 9  # the header this binding mirrors
+QTEA_ABI_VERSION = 10  # the header this binding mirrors
 QTEA_DESC_MAGIC = 0x51544541
 
 # Every function the header declares (checked by tests/test_abi.py).
@@ -49,6 +58,8 @@ EXPORTS = (
     "qtea_grouped_status", "qtea_gemm_lowbatch_noalloc",
     "qtea_packed_bytes_e4m3", "qtea_pack_e4m3", "qtea_packed_bytes_g128", "qtea_pack_g128",
     "qtea_read_ceiling", "qtea_quant_hessian", "qtea_quant_workspace_bytes", "qtea_quantize",
+    "qtea_kv_append", "qtea_kv_read", "qtea_attention_workspace_bytes", "qtea_paged_attention",
+    "qtea_verify_workspace_bytes", "qtea_verify_draft",
 )
 QTEA_LAYOUT_FP16 = 2  # residual values fp16
 QTEA_LAYOUT_E4M3 = 3  # residual values FP8 E4M3
@@ -165,6 +176,7 @@ def open_library(path: str):
     lib.qtea_quantize.restype = i32
     lib.qtea_quantize.argtypes = [vp, vp, i64, i64, ctypes.POINTER(QteaQuantParams),
                                   vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+    serving.declare(lib)
     return lib
 
 
