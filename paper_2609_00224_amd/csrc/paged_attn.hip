@@ -1,6 +1,7 @@
 // Causal attention of a batch's newest tokens over the paged cache.
 #include <math.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "serve_common.h"
@@ -139,18 +140,31 @@ __device__ __forceinline__ uint32_t finite_mask(uint32_t x) {
   return lo | hi;
 }
 
-// A pair of 16-bit values: the finite ones, and ones where a value is +inf or
-// NaN, -inf or NaN.
-struct Parts {
-  uint32_t fin, up, down;
-};
-template <class T>
-__device__ __forceinline__ Parts not_finite(uint32_t x) {
-  const uint32_t odd = ~finite_mask<T>(x), one = T::pack(1.0f, 1.0f);
-  const uint32_t mant = x & ~(0x80008000u | T::kExp | T::kExp << 16);
-  const uint32_t nan = ((mant & 0xffffu) ? 0xffffu : 0u) | ((mant >> 16) ? 0xffff0000u : 0u);
-  const uint32_t neg = ((x & 0x8000u) ? 0xffffu : 0u) | ((x >> 31) ? 0xffff0000u : 0u);
-  return {x & ~odd, one & odd & (nan | ~neg), one & odd & (nan | neg)};
+// x, opaque: what follows from it is computed where it is used and not kept
+// in registers across a loop.
+__device__ __forceinline__ int fresh(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// The cached row of a sequence's position, for one head (-1: no such page).
+__device__ __forceinline__ int64_t cached_row(const AttnArgs& a, const int32_t* table, int h, int pos) {
+  const int page = table[pos >> a.page_shift];
+  if (page < 0 || page >= a.n_pages) return -1;
+  return ((int64_t(page) * a.heads + h) << a.page_shift) + (pos & ((1 << a.page_shift) - 1));
+}
+
+// Channel c of a cached V row if it is not finite and a row sees it, for that
+// row's sum (a positive weight does not change it); else 0.
+template <int FMT, class T>
+__device__ __forceinline__ float not_finite_value(const AttnArgs& a, int64_t row, int c, bool sees) {
+  c = min(c, a.dim - 1);  // (sums of channels past the last are not used)
+  uint32_t w;
+  if constexpr (FMT == 0) w = reinterpret_cast<const uint16_t*>(a.v)[row * a.dim + c];
+  else if constexpr (FMT == 1) w = T::template e4m3<false>(a.v[row * a.dim + c], scale_of(a.vs[row * (a.dim / 32) + c / 32]));
+  else w = T::template e2m1<0>(a.v[row * (a.dim / 2) + c / 2], scale_of(a.vs[row * (a.dim / 32) + c / 32]));  // (all of a block or none)
+  const float v = float(__builtin_bit_cast(typename T::pair, w)[0]);
+  return sees && !(fabsf(v) < INFINITY) ? v : 0.0f;
 }
 
 constexpr int lds_width(int DP) { return DP < 128 ? DP : 128; }  // channels joined at a time
@@ -196,7 +210,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
   }
 
   int u = u0;
-  while (u < u1) {
+  while (u < u1 && s < a.b.n_seq) {
     const SeqWork sw = seq_work<MT>(a, s);
     if (u >= base + sw.units) {  // (a sequence without rows has no units)
       base += sw.units;
@@ -244,7 +258,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
 #pragma unroll
       for (int c = 0; c < CH; ++c) o[r][c] = f32x4{0, 0, 0, 0};
     }
-    bool bad = sw.q.bad;
+    bool bad = sw.q.bad, odd = false;
 
     const int tile_a = (sw.t0 + ua) * kWaves, tile_b = min((sw.t0 + ub) * kWaves, (hi_max + kTile - 1) / kTile);
     const int32_t* table = a.b.page_table + int64_t(s) * a.b.max_pages;
@@ -319,9 +333,10 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
         }
       }
       const bool edge = tok0 + kTile > hi_min || tok0 < lo_max;
-      bool odd_v = false;
       if (edge) {
-        // what a row does not see has no weight
+        // What a row does not see has no weight; and values that are not
+        // finite are left out, since 0 times them is not 0: not_finite_value
+        // gives them to the rows that see them.
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -334,8 +349,11 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll
-          for (int e = 0; e < CH / 2; ++e) odd_v |= finite_mask<T>(vt[j][e]) != 0xffffffffu;
-        odd_v = __ballot(odd_v) != 0;
+          for (int e = 0; e < CH / 2; ++e) {
+            const uint32_t fm = finite_mask<T>(vt[j][e]);
+            odd |= fm != 0xffffffffu && tok0 + 16 * (j / 4) + 4 * g + j % 4 < hi_max;
+            vt[j][e] &= fm;
+          }
       }
       // softmax: the running maximum moves only when a score passes it by 8 powers of two
       uint32_t pw[R][4];
@@ -370,52 +388,31 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
         for (int i = 0; i < 4; ++i) pw[r][i] = T::pack(sc[r][i / 2][2 * (i % 2)], sc[r][i / 2][2 * (i % 2) + 1]);
       }
       // V^T (16 of a lane row's channels x 32 tokens) times the weights
-      auto column = [&](int c) {
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
         u32x4 w;
 #pragma unroll
         for (int jj = 0; jj < 4; ++jj)
           w[jj] = __builtin_amdgcn_perm(vt[2 * jj + 1][c / 2], vt[2 * jj][c / 2], c % 2 ? 0x07060302u : 0x05040100u);
-        return w;
-      };
-      if (__builtin_expect(!odd_v, 1)) {
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-          const u32x4 w = column(c);
-#pragma unroll
-          for (int r = 0; r < R; ++r) o[r][c] = T::mfma16(w, u32x4{pw[r][0], pw[r][1], pw[r][2], pw[r][3]}, o[r][c]);
-        }
-      } else {
-        // A tile with values that are not finite where a row may not see
-        // them (0 * inf): products of the finite ones, then for each row and
-        // channel whether it sees a +inf or NaN, a -inf or NaN.
-        uint32_t see[R][4];
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int tok = tok0 + 16 * (i / 2) + 4 * g + 2 * (i % 2);
-            see[r][i] = T::pack(tok < hi[r] && tok >= lo[r] ? 1.0f : 0.0f, tok + 1 < hi[r] && tok + 1 >= lo[r] ? 1.0f : 0.0f);
-          }
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-          const u32x4 w = column(c);
-          u32x4 fin, up, down;
-#pragma unroll
-          for (int jj = 0; jj < 4; ++jj) {
-            const Parts p = not_finite<T>(w[jj]);
-            fin[jj] = p.fin, up[jj] = p.up, down[jj] = p.down;
-          }
+        for (int r = 0; r < R; ++r) o[r][c] = T::mfma16(w, u32x4{pw[r][0], pw[r][1], pw[r][2], pw[r][3]}, o[r][c]);
+      }
+    }
+    if (__builtin_expect(__ballot(odd) != 0, 0)) {
+      for (int t = tile_a + wave; t < tile_b; t += kWaves) {
+        const int tok0 = t * kTile;
+        if (!(tok0 + kTile > hi_min || tok0 < lo_max)) continue;
+        for (int tok = max(tok0, lo_min); tok < min(tok0 + kTile, hi_max); ++tok) {
+          const int64_t row = cached_row(a, table, h, tok);
+          if (row < 0) continue;
+          const int c0 = fresh(4 * g * CH);
 #pragma unroll
           for (int r = 0; r < R; ++r) {
-            const u32x4 sees = {see[r][0], see[r][1], see[r][2], see[r][3]};
-            const f32x4 zero = {0, 0, 0, 0};
-            o[r][c] = T::mfma16(fin, u32x4{pw[r][0], pw[r][1], pw[r][2], pw[r][3]}, o[r][c]);
-            const f32x4 plus = T::mfma16(up, sees, zero), minus = T::mfma16(down, sees, zero);
+            const bool sees = tok < hi[r] && tok >= lo[r];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              if (plus[i] > 0.0f) o[r][c][i] += INFINITY;
-              if (minus[i] > 0.0f) o[r][c][i] -= INFINITY;
-            }
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[r][c][e] += not_finite_value<FMT, T>(a, row, c0 + e * CH + c, sees);
           }
         }
       }
@@ -528,6 +525,362 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
   }
 }
 
+// ---------------------------------------------------------------------------
+// Many rows: a task is one sequence, one key/value head and 128 rows, 32 per
+// wave; the workgroup stages tiles of tokens through LDS for its four waves.
+// Where there are few tasks their tokens are split into `parts`.
+// ---------------------------------------------------------------------------
+constexpr int kTaskRows = 128;
+constexpr int kMinPart = 4;   // tiles of a part, at least
+constexpr int kMaxParts = 16; // of a task
+
+template <int DP, int FMT>
+struct Stage {
+  static constexpr int kTok = DP <= 128 ? 64 : 32;          // tokens of a tile
+  static constexpr int kBlocks = kTok / 32;
+  static constexpr int kChunk = FMT == 0 ? 8 : (FMT == 1 ? 16 : 32);  // channels of a 16-byte load
+  static constexpr int kPer = DP / kChunk;                   // chunks per token
+  static constexpr int kTotal = kTok * kPer;
+  static constexpr int kLoads = (kTotal + kThreads - 1) / kThreads;  // per thread, of K and of V
+  static constexpr int kBytes = kTok * DP * 2;               // of K (or V) in LDS
+};
+
+// Tiles in LDS, rows of DP 16-bit values, arranged so that the lanes of a read
+// fall on different banks: K's 16-byte chunks are permuted by the token (read
+// as rows of 16 bytes per lane), V's 64-byte granules (read transposed, four
+// tokens x 32 channels at a time).
+template <int DP>
+__device__ __forceinline__ uint32_t k_place(int tok, int chunk) {
+  return uint32_t(tok * (2 * DP) + ((chunk ^ (tok & (DP == 64 ? 7 : 15))) << 4));
+}
+template <int DP>
+__device__ __forceinline__ uint32_t v_place(int tok, int chunk) {
+  const int f = DP == 64 ? (tok >> 1) & 1 : tok & 3;
+  return uint32_t(tok * (2 * DP) + (((chunk >> 2) ^ f) << 6) + ((chunk & 3) << 4));
+}
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ u32x2 lds_read_transposed(const char* p) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
+}
+
+template <int DP, int FMT, class T>
+__global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attn_tile_kernel(const AttnArgs a, int parts) {
+  using ST = Stage<DP, FMT>;
+  constexpr int KT = ST::kTok, NB = ST::kBlocks, CB = DP / 32, NL = ST::kLoads;
+  __shared__ __attribute__((aligned(1024))) char s_k[2][ST::kBytes];
+  __shared__ __attribute__((aligned(1024))) char s_v[2][ST::kBytes];
+  __shared__ int s_odd, s_last;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n32 = lane & 31, half = lane >> 5;
+  const int D = a.dim, H = a.heads, G = a.group;
+  const int rowb = FMT == 0 ? 2 * D : (FMT == 1 ? D : D / 2), nb = D / 32;
+  const int capacity = a.b.max_pages << a.page_shift, pmask = (1 << a.page_shift) - 1;
+
+  // the task: heads vary fastest (a head's workgroups on one XCD, where eight
+  // divides their number), then parts, then tasks, a sequence's last first
+  const int h = blockIdx.x % H, rest = blockIdx.x / H, part = rest % parts, task = rest / parts;
+  int s = -1, base = 0;
+  for (int s0 = 0; s0 < a.b.n_seq; s0 += 64) {
+    int nq = 0;
+    if (s0 + lane < a.b.n_seq) nq = (load_seq(a.b, s0 + lane, capacity).n * G + kTaskRows - 1) / kTaskRows;
+    const int sum = wave_scan(nq);
+    const int before = __popcll(__ballot(base + sum <= task));
+    if (before < 64) {
+      s = s0 + before;
+      base += before ? __builtin_amdgcn_readlane(sum, before - 1) : 0;
+      break;
+    }
+    base += __builtin_amdgcn_readlane(sum, 63);
+  }
+  if (s < 0 || s >= a.b.n_seq) return;
+  const Seq q = load_seq(a.b, s, capacity);
+  const int rows = q.n * G, nqt = (rows + kTaskRows - 1) / kTaskRows;
+  const int r0 = (nqt - 1 - (task - base)) * kTaskRows, nrow = min(kTaskRows, rows - r0);
+  const int pos0 = q.len - q.n;
+  auto sees_to = [&](int r) { return max(0, pos0 + r / G + 1); };
+  auto sees_from = [&](int r) { return a.window > 0 ? max(0, pos0 + r / G + 1 - a.window) : 0; };
+  const int hi_max = sees_to(r0 + nrow - 1), lo_min = sees_from(r0);
+  const int hi_min = sees_to(r0), lo_max = sees_from(r0 + nrow - 1);
+
+  const int t_first = lo_min / KT, n_tiles = max(0, (hi_max + KT - 1) / KT - t_first);
+  const int used = max(1, min(parts, n_tiles / kMinPart));  // parts with work
+  if (part >= used) return;
+  const int per_part = (n_tiles + used - 1) / used;
+  const int ta = t_first + part * per_part, tb = min(t_first + n_tiles, ta + per_part);
+
+  // this wave's rows
+  const int wr0 = r0 + 32 * wave, wrow = min(32, r0 + nrow - wr0);  // (possibly none)
+  const bool ok = n32 < wrow;
+  const int my_r = ok ? wr0 + n32 : r0, my_i = my_r / G;
+  const uint16_t* qp = a.q + (int64_t(q.first) + my_i) * a.q_stride + int64_t(h * G + (my_r - my_i * G)) * D;
+  u32x4 qf[DP / 16];
+#pragma unroll
+  for (int j = 0; j < DP / 16; ++j) {
+    const int c = 16 * j + 8 * half;
+    qf[j] = u32x4{0, 0, 0, 0};
+    if (ok && c < D) qf[j] = *reinterpret_cast<const u32x4*>(qp + c);
+  }
+  const int hi = ok ? sees_to(my_r) : 0, lo = ok ? sees_from(my_r) : 0;
+  const int w_hi_max = wrow > 0 ? sees_to(wr0 + wrow - 1) : 0, w_lo_min = wrow > 0 ? sees_from(wr0) : 0;
+  const int w_hi_min = wrow > 0 ? sees_to(wr0) : 0, w_lo_max = wrow > 0 ? sees_from(wr0 + wrow - 1) : 0;
+
+  f32x16 o[CB];
+#pragma unroll
+  for (int c = 0; c < CB; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[c][i] = 0.0f;
+  float m = -INFINITY, l = 0.0f;
+
+  // staging: this thread's chunks of a tile
+  const int32_t* table = a.b.page_table + int64_t(s) * a.b.max_pages;
+  u32x4 rk[NL], rv[NL];
+  uint32_t sk[NL], sv[NL];
+  int pg[NL];
+  auto chunk_of = [&](int p, int& tok, int& cc) {
+    const int idx = tid + kThreads * p;
+    tok = idx / ST::kPer, cc = idx % ST::kPer;
+    return ST::kTotal % kThreads == 0 || idx < ST::kTotal;
+  };
+  auto pages = [&](int t) {  // the pages of tile t's chunks (past the end: of the last token)
+#pragma unroll
+    for (int p = 0; p < NL; ++p) {
+      int tok, cc;
+      chunk_of(p, tok, cc);
+      pg[p] = table[min(t * KT + min(tok, KT - 1), max(hi_max - 1, 0)) >> a.page_shift];
+    }
+  };
+  auto load = [&](int t) {
+#pragma unroll
+    for (int p = 0; p < NL; ++p) {
+      int tok, cc;
+      const bool in = chunk_of(p, tok, cc);
+      const int at = min(t * KT + min(tok, KT - 1), max(hi_max - 1, 0)), c = cc * ST::kChunk < D ? cc * ST::kChunk : 0;
+      const int page = pg[p] < 0 || pg[p] >= a.n_pages ? 0 : pg[p];
+      const int64_t row = ((int64_t(page) * H + h) << a.page_shift) + (at & pmask);
+      const int64_t off = row * rowb + (FMT == 0 ? 2 * c : (FMT == 1 ? c : c / 2));
+      if (in) {
+        rk[p] = *reinterpret_cast<const u32x4*>(a.k + off);
+        rv[p] = *reinterpret_cast<const u32x4*>(a.v + off);
+        if constexpr (FMT != 0) sk[p] = a.ks[row * nb + c / 32], sv[p] = a.vs[row * nb + c / 32];
+      }
+      if (pg[p] != page) sk[p] = 1u << 16;  // no such page: what sees it becomes NaN
+      else if constexpr (FMT == 0) sk[p] = 0;
+    }
+  };
+  auto store = [&](int t, int buf) {
+    const bool edge = t * KT + KT > hi_min || t * KT < lo_max;
+    bool odd = false;
+#pragma unroll
+    for (int p = 0; p < NL; ++p) {
+      int tok, cc;
+      if (!chunk_of(p, tok, cc)) continue;
+      const int at = t * KT + tok;
+      const bool none = cc * ST::kChunk >= D;  // channels that pad the tile
+      const bool gone = (sk[p] >> 16) != 0;
+#pragma unroll
+      for (int i = 0; i < ST::kChunk / 8; ++i) {
+        const uint32_t wk[4] = {rk[p][0], rk[p][1], rk[p][2], rk[p][3]}, wv[4] = {rv[p][0], rv[p][1], rv[p][2], rv[p][3]};
+        uint32_t k4[4], v4[4];
+        decode_words<FMT, T>(wk, i, FMT ? scale_of(sk[p] & 255u) : 1.0f, k4);
+        decode_words<FMT, T>(wv, i, FMT ? scale_of(sv[p]) : 1.0f, v4);
+        if (none || (edge && at >= hi_max)) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) k4[e] = v4[e] = 0;
+        } else if (gone) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) k4[e] = 0x7fff7fffu, v4[e] = 0;
+        }
+        if (edge) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t fm = finite_mask<T>(v4[e]);
+            odd |= fm != 0xffffffffu;
+            v4[e] &= fm;
+          }
+        }
+        const int c8 = cc * (ST::kChunk / 8) + i;
+        *reinterpret_cast<u32x4*>(&s_k[buf][k_place<DP>(tok, c8)]) = u32x4{k4[0], k4[1], k4[2], k4[3]};
+        *reinterpret_cast<u32x4*>(&s_v[buf][v_place<DP>(tok, c8)]) = u32x4{v4[0], v4[1], v4[2], v4[3]};
+      }
+    }
+    if (odd) s_odd = 1;
+  };
+
+  if (tid == 0) s_odd = 0;
+  __syncthreads();
+  if (ta < tb) {
+    pages(ta);
+    load(ta);
+    if (ta + 1 < tb) pages(ta + 1);
+    store(ta, 0);
+    if (ta + 1 < tb) load(ta + 1);
+    if (ta + 2 < tb) pages(ta + 2);
+  }
+  __syncthreads();
+
+  const uint32_t k_at = k_place<DP>(n32, half);
+  const uint32_t v_at = v_place<DP>(4 * half + ((lane >> 2) & 3), 2 * ((lane >> 4) & 1)) + 8 * (lane & 3);
+  for (int t = ta; t < tb; ++t) {
+    const int buf = (t - ta) & 1, tok0 = t * KT;
+    if (tok0 < w_hi_max && tok0 + KT > w_lo_min) {
+      const char* kb = s_k[buf];
+      const char* vb = s_v[buf];
+      f32x16 sc[NB];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[b][i] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < DP / 16; ++j) {
+          const u32x4 kf = *reinterpret_cast<const u32x4*>(kb + ((k_at ^ uint32_t(j << 5)) + b * (32 * 2 * DP)));
+          sc[b] = T::mfma32(kf, qf[j], sc[b]);
+        }
+      }
+      const bool edge = tok0 + KT > w_hi_min || tok0 < w_lo_max;
+      if (edge) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int tok = tok0 + 32 * b + 8 * (i >> 2) + 4 * half + (i & 3);
+            if (tok >= hi || tok < lo) sc[b][i] = -INFINITY;
+          }
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[b][i]);
+      if (__ballot(top * a.scale > m + 8.0f)) {
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float now = fmaxf(m, top * a.scale);
+        const float f = m == now ? 1.0f : exp2f(m - now);
+        m = now;
+        l *= f;
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[c][i] *= f;
+      }
+      const float off = (m == -INFINITY ? 0.0f : -m) + T::kLift;
+      uint32_t pw[NB][8];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          sc[b][i] = __builtin_amdgcn_exp2f(fmaf(sc[b][i], a.scale, off));
+          l += sc[b][i];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) pw[b][i] = T::pack(sc[b][2 * i], sc[b][2 * i + 1]);
+      }
+      auto column = [&](int c, int st) {
+        const char* p = vb + ((v_at ^ uint32_t(c << 6)) + st * (16 * 2 * DP));
+        const u32x2 x = lds_read_transposed(p), y = lds_read_transposed(p + 8 * 2 * DP);
+        return u32x4{x[0], x[1], y[0], y[1]};
+      };
+#pragma unroll
+      for (int st = 0; st < 2 * NB; ++st) {
+        const uint32_t* w = &pw[st >> 1][4 * (st & 1)];
+#pragma unroll
+        for (int c = 0; c < CB; ++c) o[c] = T::mfma32(column(c, st), u32x4{w[0], w[1], w[2], w[3]}, o[c]);
+      }
+    }
+    if (t + 1 < tb) {
+      store(t + 1, buf ^ 1);
+      if (t + 2 < tb) load(t + 2);
+      if (t + 3 < tb) pages(t + 3);
+    }
+    __syncthreads();
+  }
+
+  if (__builtin_expect(s_odd, 0)) {  // (as in attn_rows_kernel)
+    for (int t = ta; t < tb; ++t) {
+      const int tok0 = t * KT;
+      if (!(tok0 + KT > hi_min || tok0 < lo_max)) continue;
+      for (int tok = max(tok0, lo_min); tok < min(tok0 + KT, hi_max); ++tok) {
+        const int64_t row = cached_row(a, table, h, tok);
+        if (row < 0) continue;
+        const bool sees = tok < hi && tok >= lo;
+        const int c0 = fresh(4 * half);
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[c][i] += not_finite_value<FMT, T>(a, row, c0 + 32 * c + 8 * (i >> 2) + (i & 3), sees);
+      }
+    }
+  }
+  l += __shfl_xor(l, 32);
+  if (q.bad) l = __builtin_nanf("");
+  uint16_t* dst = a.out + (int64_t(q.first) + my_i) * a.out_stride + int64_t(h * G + (my_r - my_i * G)) * D;
+  if (used == 1) {
+    const float inv = pos0 + my_i < 0 && l == 0.0f ? 0.0f : 1.0f / l;
+    if (ok) {
+#pragma unroll
+      for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int ch = 32 * c + 8 * i + 4 * half;
+          if (ch < D)
+            *reinterpret_cast<u32x2*>(dst + ch) = u32x2{T::pack(o[c][4 * i] * inv, o[c][4 * i + 1] * inv), T::pack(o[c][4 * i + 2] * inv, o[c][4 * i + 3] * inv)};
+        }
+    }
+    return;
+  }
+  // The task's parts: the last workgroup to arrive sums them, in part order.
+  const int id = task * H + h;
+  const int64_t slot0 = int64_t(id) * parts;
+  float* mine = a.part + (slot0 + part) * (kTaskRows * DP) + (32 * wave + n32) * DP;
+  float* ml = a.part_ml + (slot0 + part) * (2 * kTaskRows) + 32 * wave + n32;
+  if (ok) {
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int ch = 32 * c + 8 * (i >> 2) + 4 * half + (i & 3);
+        if (ch < D) qtea_detail::store_coherent(mine + ch, o[c][i]);
+      }
+    if (half == 0) {
+      qtea_detail::store_coherent(ml, m);
+      qtea_detail::store_coherent(ml + kTaskRows, l);
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(0);  // the part is complete before its arrival is counted
+  __syncthreads();
+  if (tid == 0) {
+    const uint32_t before = __hip_atomic_fetch_add(a.counters + id, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const bool last = before == uint32_t(used - 1);
+    if (last) __hip_atomic_store(a.counters + id, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    s_last = last;
+  }
+  __syncthreads();
+  if (!s_last) return;
+  for (int e = tid; e < nrow * (DP / 4); e += kThreads) {
+    const int row = e / (DP / 4), ch = (e % (DP / 4)) * 4;
+    if (ch >= D) continue;
+    float M = -INFINITY, L = 0.0f;
+    f32x4 acc = {0, 0, 0, 0};
+    for (int w = 0; w < used; ++w) {
+      const float* pm = a.part_ml + (slot0 + w) * (2 * kTaskRows) + row;
+      const float* po = a.part + (slot0 + w) * (kTaskRows * DP) + row * DP + ch;
+      const float mw = qtea_detail::load_coherent(pm), lw = qtea_detail::load_coherent(pm + kTaskRows);
+      f32x4 ow;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) ow[i] = qtea_detail::load_coherent(po + i);
+      const float now = fmaxf(M, mw);
+      const float fa = M == now ? 1.0f : exp2f(M - now), fb = mw == now ? 1.0f : exp2f(mw - now);
+      M = now;
+      L = L * fa + lw * fb;
+      acc = acc * fa + ow * fb;
+    }
+    const int r = r0 + row, i = r / G;
+    const float inv = pos0 + i < 0 && L == 0.0f ? 0.0f : 1.0f / L;
+    uint16_t* to = a.out + (int64_t(q.first) + i) * a.out_stride + int64_t(h * G + (r - i * G)) * D + ch;
+    *reinterpret_cast<u32x2*>(to) = u32x2{T::pack(acc[0] * inv, acc[1] * inv), T::pack(acc[2] * inv, acc[3] * inv)};
+  }
+}
+
 int device_cus() {
   static std::atomic<int> known[qtea_detail::kMaxDevices];
   return qtea_detail::per_current_device(known, [](int dev) {
@@ -536,7 +889,9 @@ int device_cus() {
   });
 }
 
-// The workspace: counters, the parts' maxima and sums, the parts.
+// The workspace: counters, the parts' maxima and sums, the parts; for the
+// grid of the one kernel with two parts a workgroup, and for as many
+// workgroups of the other, one part each.
 constexpr int kRowsMax = 32;
 struct WsLayout {
   int64_t ml, part, bytes;
@@ -544,10 +899,11 @@ struct WsLayout {
 int padded_dim(int dim) { return dim <= 64 ? 64 : (dim <= 128 ? 128 : 256); }
 WsLayout ws_layout(int dim, int cus) {
   const int64_t grid = int64_t(cus) * kWgPerCu;
+  static_assert(kTaskRows >= 2 * kRowsMax, "the workspace holds either kernel's parts");
   WsLayout w;
   w.ml = (4 * grid + 255) / 256 * 256;
-  w.part = w.ml + 2 * grid * 2 * kRowsMax * 4;
-  w.bytes = w.part + 2 * grid * kRowsMax * padded_dim(dim) * 4;
+  w.part = w.ml + grid * 2 * kTaskRows * 4;
+  w.bytes = w.part + grid * kTaskRows * padded_dim(dim) * 4;
   return w;
 }
 
@@ -600,19 +956,27 @@ int qtea_paged_attention(const qtea_kv_cache* cache, const qtea_kv_batch* batch,
   a.counters = reinterpret_cast<uint32_t*>(ws);
   a.part_ml = reinterpret_cast<float*>(ws + wl.ml);
   a.part = reinterpret_cast<float*>(ws + wl.part);
-  const dim3 grid(cus * kWgPerCu), block(kThreads);
+  const dim3 block(kThreads);
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  const bool two = D <= 128 && rows > int64_t(16) * batch->n_seq;
+  // The kernel by a sequence's rows on average (a call's lengths are only known on the device).
+  const bool many = rows > int64_t(kRowsMax) * batch->n_seq, two = D <= 128 && rows > int64_t(16) * batch->n_seq;
+  const int64_t tasks = rows / kTaskRows + batch->n_seq, grid = int64_t(cus) * kWgPerCu;  // (tasks per head, at most)
+  const int parts = int(std::max<int64_t>(1, std::min<int64_t>(grid / (tasks * H), kMaxParts)));
+  if (many && tasks * H * parts > INT32_MAX) return QTEA_ERR_INVALID_ARG;
   auto launch = [&](auto dp, auto fmt, auto ty) {
     constexpr int DP = decltype(dp)::value, FMT = decltype(fmt)::value;
     using T = decltype(ty);
+    if (many) {
+      hipLaunchKernelGGL((attn_tile_kernel<DP, FMT, T>), dim3(uint32_t(tasks * H * parts)), block, 0, st, a, parts);
+      return;
+    }
     if constexpr (DP <= 128) {
       if (two) {
-        hipLaunchKernelGGL((attn_rows_kernel<DP, FMT, T, 2>), grid, block, 0, st, a);
+        hipLaunchKernelGGL((attn_rows_kernel<DP, FMT, T, 2>), dim3(uint32_t(grid)), block, 0, st, a);
         return;
       }
     }
-    hipLaunchKernelGGL((attn_rows_kernel<DP, FMT, T, 1>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((attn_rows_kernel<DP, FMT, T, 1>), dim3(uint32_t(grid)), block, 0, st, a);
   };
   auto with_type = [&](auto dp, auto fmt) {
     if (type == QTEA_F16) launch(dp, fmt, F16());
