@@ -9,11 +9,11 @@
 namespace qtea_serve {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
-constexpr int kTile = 32;              // tokens of one step of a wave
-constexpr int kUnit = kTile * kWaves;  // tokens of one step of a workgroup
-constexpr int kWgPerCu = 2;
+constexpr int kTile = 32;      // tokens of one step of a wave (few rows)
+constexpr int kWaves = 4, kRowThreads = 64 * kWaves;  // of a workgroup (few rows)
+constexpr int kUnit = kTile * kWaves;
+constexpr int kThreads = 256;  // of a workgroup of the kernel for many rows
+constexpr int kWgPerCu = 2;    // of those
 
 struct AttnArgs {
   const uint8_t* k;
@@ -24,7 +24,7 @@ struct AttnArgs {
   uint16_t* out;
   int64_t q_stride, out_stride;  // elements
   Batch b;
-  int32_t heads, group, dim, page_shift, n_pages, window;
+  int32_t heads, group, dim, page_shift, n_pages, window, max_slots;
   float scale;       // times log2(e)
   uint32_t* counters;
   float* part;       // partial rows
@@ -33,17 +33,18 @@ struct AttnArgs {
 
 // ---------------------------------------------------------------------------
 // Few rows: a task is one sequence, one key/value head and up to 16 R rows
-// (new tokens x the query heads that share the head).  Its tokens are split
-// over the waves of a workgroup, and the tasks' units of 128 tokens, one
-// after another, in equal runs over the workgroups.
+// (new tokens x the query heads that share the head).  A task's tokens are
+// split into chunks, one to a workgroup, so that every CU has its workgroups
+// busy for about as long; a chunk's tokens are dealt to the waves, 32 at a
+// time, and each wave keeps its own sums until the end.
 // ---------------------------------------------------------------------------
 
-// The work of sequence s: `nqt` row tasks per head, each of `cnt` units from
-// unit t0 on (the same for all: what its first row sees starts there, what
-// the last one sees ends there).
+// The work of sequence s: `nqt` row tasks per head, each of `cnt` units of
+// tokens from unit t0 on (the same for all: what its first row sees starts
+// there, what the last one sees ends there).
 struct SeqWork {
   Seq q;
-  int t0, cnt, nqt, units;
+  int t0, cnt, nqt, tasks;
 };
 
 template <int MT>
@@ -55,27 +56,22 @@ __device__ __forceinline__ SeqWork seq_work(const AttnArgs& a, int s) {
   w.t0 = lo / kUnit;
   w.cnt = max(1, (w.q.len + kUnit - 1) / kUnit - w.t0);
   w.nqt = (w.q.n * a.group + MT - 1) / MT;
-  w.units = w.nqt * w.cnt * a.heads;
+  w.tasks = w.nqt * a.heads;
   return w;
 }
 
+// Chunks of a task of cnt units, for chunks of about 1 / rate units.
+__device__ __forceinline__ int chunks_of(int cnt, float rate) { return max(1, int(__builtin_ceilf(float(cnt) * rate))); }
+
 // Inclusive sum over the wave's lanes.
 __device__ __forceinline__ int wave_scan(int x) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // from 1, 2, 4, 8 lanes below in the row of 16
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // a row's last lane to the next row
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to the upper half
   return x;
-}
-
-// Units before workgroup w's run, of W units over G workgroups; and the
-// workgroup that has unit u.
-__device__ __forceinline__ int run_first(int w, int W, int G) { return w * (W / G) + min(w, W % G); }
-__device__ __forceinline__ int run_owner(int u, int W, int G) {
-  const int q = W / G, r = W % G, big = r * (q + 1);
-  return u < big ? u / (q + 1) : r + (u - big) / q;
 }
 
 // A lane's registers of one tile: the K codes of its token in both 16-token
@@ -89,10 +85,11 @@ struct Tile {
   static constexpr int kChunks = DP / (4 * kChunk);                         // K loads per half
   static constexpr int kCH = DP / 16;                                       // channels per lane in V
   static constexpr int kVWords = (kCH / 2 + kShrink - 1) / kShrink;         // words of V per token
+  static constexpr int kScaleWords = DP <= 128 ? 1 : 2;                     // words of a token's K scales
   uint32_t k[2][kKWords];
   uint32_t v[8][kVWords];
-  uint32_t ks[2][kChunks];
-  uint32_t vs[8];
+  uint32_t ks[2][kScaleWords];  // scale bytes of the token, block b in byte b
+  uint32_t vs[8];               // the word of the token's scale bytes that holds this lane's
 };
 
 template <int N>
@@ -100,15 +97,15 @@ __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w) {
   if constexpr (N % 4 == 0) {
 #pragma unroll
     for (int i = 0; i < N; i += 4) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(p + 4 * i);
+      const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + 4 * i));
 #pragma unroll
       for (int j = 0; j < 4; ++j) w[i + j] = x[j];
     }
   } else if constexpr (N == 2) {
-    const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+    const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
     w[0] = x[0], w[1] = x[1];
   } else {
-    w[0] = *reinterpret_cast<const uint32_t*>(p);
+    w[0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p));
   }
 }
 
@@ -132,12 +129,54 @@ __device__ __forceinline__ void decode_words(const uint32_t* w, int i, float s, 
   }
 }
 
+// Channels 2 i, 2 i + 1 of the codes in w.
+template <int FMT, class T>
+__device__ __forceinline__ uint32_t decode_pair(const uint32_t* w, int i, float s) {
+  if constexpr (FMT == 0) return w[i];
+  else if constexpr (FMT == 1) return i % 2 ? T::template e4m3<true>(w[i / 2], s) : T::template e4m3<false>(w[i / 2], s);
+  else {
+    switch (i % 4) {
+      case 0: return T::template e2m1<0>(w[i / 4], s);
+      case 1: return T::template e2m1<1>(w[i / 4], s);
+      case 2: return T::template e2m1<2>(w[i / 4], s);
+      default: return T::template e2m1<3>(w[i / 4], s);
+    }
+  }
+}
+
+// The factor of the scale byte at bit `shift` of a word.
+__device__ __forceinline__ float scale_at(uint32_t word, int shift) { return scale_of(__builtin_amdgcn_ubfe(word, shift, 8)); }
+
 // A 16-bit channel pair is not finite in either half.
 template <class T>
 __device__ __forceinline__ uint32_t finite_mask(uint32_t x) {
   const uint32_t lo = (x & T::kExp) == T::kExp ? 0u : 0xffffu;
   const uint32_t hi = ((x >> 16) & T::kExp) == T::kExp ? 0u : 0xffff0000u;
   return lo | hi;
+}
+
+// Zeroes the values of N words of V codes that are not finite; whether there
+// were any.  (E4M3: NaN codes, and blocks of a NaN scale, E2M1's only kind.)
+template <int FMT, class T, int N>
+__device__ __forceinline__ bool drop_not_finite(uint32_t* w, uint32_t& scales, int shift) {
+  uint32_t keep_all = 0xffffffffu, lost = 0;
+  if constexpr (FMT != 0) {
+    keep_all = __builtin_amdgcn_ubfe(scales, shift, 8) == 255u ? 0u : 0xffffffffu;
+    scales &= keep_all;
+    lost = ~keep_all;
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    uint32_t keep = keep_all;
+    if constexpr (FMT == 0) keep = finite_mask<T>(w[i]);
+    if constexpr (FMT == 1) {
+      const uint32_t nan = (((w[i] & 0x7f7f7f7fu) + 0x01010101u) >> 7) & 0x01010101u;  // per byte: all ones below the sign
+      keep &= ~(nan * 255u);
+    }
+    lost |= ~keep;
+    w[i] &= keep;
+  }
+  return lost != 0;
 }
 
 // x, opaque: what follows from it is computed where it is used and not kept
@@ -154,71 +193,189 @@ __device__ __forceinline__ int64_t cached_row(const AttnArgs& a, const int32_t* 
   return ((int64_t(page) * a.heads + h) << a.page_shift) + (pos & ((1 << a.page_shift) - 1));
 }
 
-// Channel c of a cached V row if it is not finite and a row sees it, for that
-// row's sum (a positive weight does not change it); else 0.
+// Channel c of a cached V row if it is not finite, else 0 (for the sum of a row
+// that sees it: a positive weight does not change it).
 template <int FMT, class T>
-__device__ __forceinline__ float not_finite_value(const AttnArgs& a, int64_t row, int c, bool sees) {
+__device__ __forceinline__ float not_finite_value(const AttnArgs& a, int64_t row, int c) {
   c = min(c, a.dim - 1);  // (sums of channels past the last are not used)
   uint32_t w;
   if constexpr (FMT == 0) w = reinterpret_cast<const uint16_t*>(a.v)[row * a.dim + c];
   else if constexpr (FMT == 1) w = T::template e4m3<false>(a.v[row * a.dim + c], scale_of(a.vs[row * (a.dim / 32) + c / 32]));
   else w = T::template e2m1<0>(a.v[row * (a.dim / 2) + c / 2], scale_of(a.vs[row * (a.dim / 32) + c / 32]));  // (all of a block or none)
   const float v = float(__builtin_bit_cast(typename T::pair, w)[0]);
-  return sees && !(fabsf(v) < INFINITY) ? v : 0.0f;
+  return fabsf(v) < INFINITY ? 0.0f : v;
+}
+
+__device__ __forceinline__ void store_coherent2(float* p, float x, float y) {
+  const f32x2 v = {x, y};
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), __builtin_bit_cast(uint64_t, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ f32x2 load_coherent2(const float* p) {
+  return __builtin_bit_cast(f32x2, __hip_atomic_load(reinterpret_cast<uint64_t*>(const_cast<float*>(p)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+
+// A row's running maximum, sum and four channels, and those of other tokens.
+struct Joined {
+  float M = -INFINITY, L = 0.0f;
+  f32x4 acc = {0, 0, 0, 0};
+  __device__ __forceinline__ void add(float m, float l, f32x4 o) {
+    const float now = fmaxf(M, m);
+    const float fa = M == now ? 1.0f : __builtin_amdgcn_exp2f(M - now), fb = m == now ? 1.0f : __builtin_amdgcn_exp2f(m - now);
+    M = now;
+    L = L * fa + l * fb;
+    acc = acc * fa + o * fb;
+  }
+};
+
+// Counts this workgroup's arrival; whether it is the last of n.
+__device__ __forceinline__ bool last_to_arrive(uint32_t* counter, int n, int* s_last) {
+  __builtin_amdgcn_s_waitcnt(0);  // what it stored is complete before its arrival is counted
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const uint32_t before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const bool last = before == uint32_t(n - 1);
+    if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *s_last = last;
+  }
+  __syncthreads();
+  return *s_last;
+}
+
+constexpr int kJoin = 12;  // parts joined at once
+
+// Joins the parts of a task's rows in part order, by the whole workgroup: four
+// channels a thread, and with few rows the parts dealt to groups of threads,
+// whose results are joined in group order.  The parts are `step` slots apart.
+// `give(row, channel, result)` takes the results.  `lds`: 6 floats a thread.  Every load of a
+// batch is on its way before the first is used: they come from the other
+// XCDs' stores, past this one's L2.
+template <int DP, int MT, int THREADS, class Give>
+__device__ __forceinline__ void join_parts(const AttnArgs& a, const float* part_ml, int64_t slot0, int step, int n_parts, int nrow, float* lds, Give give) {
+  constexpr int kBatch = 8;
+  const int tid = threadIdx.x;
+  const int quads = a.dim / 4, items = nrow * quads;
+  const int groups = max(1, min(THREADS / items, n_parts)), grp = groups > 1 ? tid / items : 0;
+  for (int e = tid - grp * items; e < items && grp < groups; e += groups > 1 ? items : THREADS) {
+    const int row = e / quads, ch = (e - row * quads) * 4;
+    Joined j;
+    for (int w0 = grp; w0 < n_parts; w0 += groups * kBatch) {
+      float mw[kBatch], lw[kBatch];
+      f32x2 x[kBatch], y[kBatch];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const int64_t sl = slot0 + step * min(w0 + groups * i, n_parts - 1);
+        const float* pm = part_ml + sl * (2 * MT) + row;
+        const float* po = a.part + sl * (MT * DP) + row * DP + ch;
+        mw[i] = qtea_detail::load_coherent(pm), lw[i] = qtea_detail::load_coherent(pm + MT);
+        x[i] = load_coherent2(po), y[i] = load_coherent2(po + 2);
+      }
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i)
+        if (w0 + groups * i < n_parts) j.add(mw[i], lw[i], f32x4{x[i][0], x[i][1], y[i][0], y[i][1]});
+    }
+    if (groups > 1) {
+      *reinterpret_cast<f32x4*>(lds + 4 * tid) = j.acc;
+      lds[4 * THREADS + 2 * tid] = j.M, lds[4 * THREADS + 2 * tid + 1] = j.L;
+    } else {
+      give(row, ch, j);
+    }
+  }
+  if (groups > 1) {
+    __syncthreads();
+    if (tid < items) {
+      Joined j;
+      for (int k = 0; k < groups; ++k) {
+        const int t = tid + k * items;
+        j.add(lds[4 * THREADS + 2 * t], lds[4 * THREADS + 2 * t + 1], *reinterpret_cast<const f32x4*>(lds + 4 * t));
+      }
+      const int row = tid / quads;
+      give(row, (tid - row * quads) * 4, j);
+    }
+  }
 }
 
 constexpr int lds_width(int DP) { return DP < 128 ? DP : 128; }  // channels joined at a time
 
-template <int DP, int FMT, class T, int R>
-__global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a) {
+constexpr float kMinUnits = 2.0f;  // of a chunk: what joining two costs
+// Workgroups per CU, each of one wave per SIMD: as many as have the registers
+// for a tile on the way beside their sums.
+constexpr int rows_per_cu(int DP, int FMT, int R) { return DP == 256 || R == 2 ? 1 : (FMT == 0 && DP == 128 ? 2 : 3); }
+
+// EX: the heads have DP channels; else they have fewer, and what lies past
+// them is read from the first channels instead (queries are 0 there, and sums
+// not used).
+template <int DP, int FMT, class T, int R, bool EX>
+__global__ __launch_bounds__(kRowThreads, rows_per_cu(DP, FMT, R)) void attn_rows_kernel(const AttnArgs a) {
   using TL = Tile<DP, FMT>;
   constexpr int MT = 16 * R;
   constexpr int CH = TL::kCH, CW = lds_width(DP), CS = CW + 4;  // (+ 4: rows on other banks)
   __shared__ float s_o[kWaves][16][CS];
-  __shared__ float s_m[kWaves][MT], s_l[kWaves][MT];
-  __shared__ int s_last;
+  __shared__ float s_m[kWaves][MT], s_l[kWaves][MT], s_sum[MT];
+  __shared__ int s_last, s_odd;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n16 = lane & 15, g = lane >> 4;
-  const int D = a.dim, H = a.heads, G = a.group;
-  const int rowb = FMT == 0 ? 2 * D : (FMT == 1 ? D : D / 2), nb = D / 32;
+  const int D = EX ? DP : a.dim, H = a.heads, G = a.group;
+  const uint32_t rowb = FMT == 0 ? 2 * D : (FMT == 1 ? D : D / 2), nb = D / 32;
   const int pmask = (1 << a.page_shift) - 1;
+  // where this lane's codes and scales are in a half's rows
+  auto code_bytes = [](uint32_t channels) { return FMT == 0 ? 2 * channels : (FMT == 1 ? channels : channels / 2); };
+  const uint32_t k_lane = n16 * rowb, k_at = k_lane + code_bytes(!EX && g * TL::kChunk >= D ? 0 : g * TL::kChunk);
+  const uint32_t v_at = 4 * g * rowb + code_bytes(!EX && n16 * CH >= D ? 0 : n16 * CH);
+  // where this lane's scale bytes are in their words
+  const int k_shift = 8 * (g * TL::kChunk / 32), v_shift = 8 * (n16 * CH / 32 % 4);
 
-  // the call's units, and the sequence where this workgroup's run begins
-  // (each wave for itself: no barrier)
-  int W = 0;
+  __builtin_amdgcn_s_setprio(3);
+  // The call's chunks (each wave for itself: no barrier).  Their size: the
+  // smallest of 64 candidates, from an equal share of all units for every
+  // workgroup to three times that, whose chunks are no more than the
+  // workgroups; for more sequences than a wave has lanes, half as much again
+  // as the share (what is over waits for a workgroup to be free).
+  const bool one_wave = a.b.n_seq <= 64;  // of sequences, a lane each
+  SeqWork mine = {};
+  int W = 0;  // units of all tasks
   for (int s0 = 0; s0 < a.b.n_seq; s0 += 64) {
-    const int u = s0 + lane < a.b.n_seq ? seq_work<MT>(a, s0 + lane).units : 0;
-    W += __builtin_amdgcn_readlane(wave_scan(u), 63);
+    mine = SeqWork{};
+    if (s0 + lane < a.b.n_seq) mine = seq_work<MT>(a, s0 + lane);
+    W += __builtin_amdgcn_readlane(wave_scan(mine.cnt * mine.tasks), 63);
   }
-  const int NG = min(int(gridDim.x), W);
-  // neighbouring runs on one XCD: tasks of one head share its cached bytes
-  int wg = blockIdx.x;
-  if (gridDim.x % 8 == 0) wg = (wg & 7) * (gridDim.x / 8) + (wg >> 3);
-  if (wg >= NG) return;
-  const int u0 = run_first(wg, W, NG), u1 = run_first(wg + 1, W, NG);
-  int s = 0, base = 0;
-  for (int s0 = 0; s0 < a.b.n_seq; s0 += 64) {
-    const int u = s0 + lane < a.b.n_seq ? seq_work<MT>(a, s0 + lane).units : 0;
-    const int sum = wave_scan(u);
-    const int before = __popcll(__ballot(base + sum <= u0));
-    if (before < 64) {
-      s = s0 + before;
-      base += before ? __builtin_amdgcn_readlane(sum, before - 1) : 0;
-      break;
-    }
-    base += __builtin_amdgcn_readlane(sum, 63);
+  const float share = fmaxf(float(W) / float(gridDim.x), kMinUnits);
+  float rate = 1.0f / (share * 1.5f);
+  if (one_wave) {
+    const float r = 1.0f / (share * (1.0f + float(lane) * (2.0f / 63.0f)));
+    int chunks = 0;
+    for (int j = 0; j < a.b.n_seq; ++j) chunks += __builtin_amdgcn_readlane(mine.tasks, j) * chunks_of(__builtin_amdgcn_readlane(mine.cnt, j), r);
+    const uint64_t fit = __ballot(chunks <= int(gridDim.x));
+    rate = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(r), fit ? __builtin_ctzll(fit) : 63));
   }
 
-  int u = u0;
-  while (u < u1 && s < a.b.n_seq) {
-    const SeqWork sw = seq_work<MT>(a, s);
-    if (u >= base + sw.units) {  // (a sequence without rows has no units)
-      base += sw.units;
-      ++s;
-      continue;
+  for (int id = blockIdx.x;; id += gridDim.x) {
+    // this chunk's sequence; chunks of split tasks before it have the first slots
+    int s = -1, base = 0, slot0 = 0;
+    SeqWork sw;
+    for (int s0 = 0; s0 < a.b.n_seq; s0 += 64) {
+      if (!one_wave) {
+        mine = SeqWork{};
+        if (s0 + lane < a.b.n_seq) mine = seq_work<MT>(a, s0 + lane);
+      }
+      const int k = chunks_of(mine.cnt, rate), sum = wave_scan(k * mine.tasks), split = wave_scan(k > 1 ? k * mine.tasks : 0);
+      const int before = __popcll(__ballot(base + sum <= id));
+      if (before < 64) {
+        s = s0 + before;
+        base += before ? __builtin_amdgcn_readlane(sum, before - 1) : 0;
+        slot0 += before ? __builtin_amdgcn_readlane(split, before - 1) : 0;
+        auto of = [&](int x) { return __builtin_amdgcn_readlane(x, before); };
+        sw = SeqWork{{of(mine.q.first), of(mine.q.n), of(mine.q.len), of(mine.q.bad) != 0}, of(mine.t0), of(mine.cnt), of(mine.nqt), of(mine.tasks)};
+        break;
+      }
+      base += __builtin_amdgcn_readlane(sum, 63);
+      slot0 += __builtin_amdgcn_readlane(split, 63);
     }
-    const int rel = u - base, task = rel / sw.cnt, ua = rel - task * sw.cnt;
-    const int ub = min(sw.cnt, ua + (u1 - u));  // units [ua, ub) of the task
+    if (s < 0 || s >= a.b.n_seq) return;
+    const int parts = __builtin_amdgcn_readfirstlane(chunks_of(sw.cnt, rate)), task = (id - base) / parts, part = (id - base) - task * parts;
+    const int per = sw.cnt / parts, more = sw.cnt - per * parts;
+    const int ua = part * per + min(part, more), ub = ua + per + (part < more ? 1 : 0);  // units [ua, ub) of the task
+    // (starts that decrease can make the counts above overflow: not past the operands or the workspace)
+    if (task < 0 || task >= sw.tasks || slot0 < 0 || (parts > 1 && slot0 + (task + 1) * parts > a.max_slots)) return;
     const int h = task / sw.nqt, r0 = (task - h * sw.nqt) * MT;
     const int rows = sw.q.n * G, nrow = min(MT, rows - r0);
     const int64_t token_row0 = sw.q.first;
@@ -259,43 +416,119 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
       for (int c = 0; c < CH; ++c) o[r][c] = f32x4{0, 0, 0, 0};
     }
     bool bad = sw.q.bad, odd = false;
+    if (tid == 0) s_odd = 0;  // (read after the barriers below)
 
     const int tile_a = (sw.t0 + ua) * kWaves, tile_b = min((sw.t0 + ub) * kWaves, (hi_max + kTile - 1) / kTile);
     const int32_t* table = a.b.page_table + int64_t(s) * a.b.max_pages;
-    for (int t = tile_a + wave; t < tile_b; t += kWaves) {
-      const int tok0 = t * kTile;
-      if (tok0 + kTile <= lo_min) continue;
-      TL x;
-      int64_t prow[2];  // cached row of the halves' first tokens
+    // The pages of this wave's next 32 tiles' halves, a lane each (a half past
+    // the end repeats the last one).
+    int t = tile_a + wave;
+    if (t < lo_min / kTile) t += (lo_min / kTile - t + kWaves - 1) / kWaves * kWaves;
+    int page = 0, page_at = 0;  // (page_at: the tile of the first lane)
+    auto half_first = [&](int t, int sub) { return min(t * kTile + 16 * sub, (hi_max - 1) & ~15); };
+    auto load_pages = [&](int from) {
+      const int tok = half_first(from + (lane >> 1) * kWaves, lane & 1);
+      page = table[tok >> a.page_shift], page_at = from;
+      const bool none = page < 0 || page >= a.n_pages;
+      // (a half below the window holds no visible token: its page may be gone)
+      bad = bad || __ballot(none && tok + 16 > lo_min) != 0;
+      if (none) page = 0;
+    };
+    // Cached rows of the halves' first tokens.
+    auto places = [&](int t, int64_t (&prow)[2]) {
+      const int k = (t - page_at) / kWaves;
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub)
+        prow[sub] = ((int64_t(__builtin_amdgcn_readlane(page, 2 * k + sub)) * H + h) << a.page_shift) + (half_first(t, sub) & pmask);
+    };
+    TL x;
+    auto load_k = [&](const int64_t (&prow)[2]) {
 #pragma unroll
       for (int sub = 0; sub < 2; ++sub) {
-        const int tok = min(tok0 + 16 * sub, (hi_max - 1) & ~15);  // (a half past the end repeats the last one)
-        int page = table[tok >> a.page_shift];
-        if (page < 0 || page >= a.n_pages) {
-          // a half below the window holds no visible token: its page may be gone
-          bad = bad || tok + 16 > lo_min;
-          page = 0;
-        }
-        prow[sub] = ((int64_t(page) * H + h) << a.page_shift) + (tok & pmask);
-      }
-#pragma unroll
-      for (int sub = 0; sub < 2; ++sub) {
-        const uint8_t* kp = a.k + prow[sub] * rowb + n16 * rowb;
-        const uint8_t* sp = FMT ? a.ks + prow[sub] * nb + n16 * nb : nullptr;
+        const uint8_t* kp = a.k + prow[sub] * rowb;
+        const uint32_t at = fresh(k_at);
 #pragma unroll
         for (int i = 0; i < TL::kChunks; ++i) {
-          const int c = i * (4 * TL::kChunk) + g * TL::kChunk, cc = c < D ? c : 0;
-          load_words<TL::kKWords / TL::kChunks>(kp + (FMT == 0 ? 2 * cc : (FMT == 1 ? cc : cc / 2)), x.k[sub] + i * (TL::kKWords / TL::kChunks));
-          if constexpr (FMT != 0) x.ks[sub][i] = sp[cc / 32];
+          constexpr int kLoad = TL::kKWords / TL::kChunks;
+          const uint8_t* from = kp + at + i * 16 * kLoad;
+          if (!EX && i * (4 * TL::kChunk) + g * TL::kChunk >= D) from = kp + k_lane;  // (past the last channel)
+          load_words<kLoad>(from, x.k[sub] + i * kLoad);
         }
+        if constexpr (FMT != 0) {
+          const uint8_t* sp = a.ks + prow[sub] * nb;
+          if constexpr (EX) {
+            const uint32_t sat = fresh(nb * n16);
+            if constexpr (DP == 64) x.ks[sub][0] = *reinterpret_cast<const uint16_t*>(sp + sat);
+            else load_words<TL::kScaleWords>(sp + sat, x.ks[sub]);
+          } else {
+#pragma unroll
+            for (int w = 0; w < TL::kScaleWords; ++w) x.ks[sub][w] = 0;
+#pragma unroll
+            for (int i = 0; i < TL::kChunks; ++i) {
+              const int c = i * (4 * TL::kChunk) + g * TL::kChunk;
+              x.ks[sub][i * TL::kChunk / 32] |= uint32_t(sp[nb * n16 + uint32_t(c < D ? c : 0) / 32]) << (8 * (i * TL::kChunk / 8 % 4) + k_shift);
+            }
+          }
+        }
+      }
+    };
+    auto load_v = [&](const int64_t (&prow)[2]) {
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub) {
+        const uint8_t* vp = a.v + prow[sub] * rowb;
+        const uint32_t at = fresh(v_at);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const int c = n16 * CH < D ? n16 * CH : 0;
-          const uint8_t* vp = a.v + prow[sub] * rowb + (4 * g + j) * rowb + (FMT == 0 ? 2 * c : (FMT == 1 ? c : c / 2));
-          if constexpr (FMT == 2 && CH == 4) x.v[4 * sub + j][0] = *reinterpret_cast<const uint16_t*>(vp);
-          else load_words<TL::kVWords>(vp, x.v[4 * sub + j]);
-          if constexpr (FMT != 0) x.vs[4 * sub + j] = a.vs[prow[sub] * nb + (4 * g + j) * nb + c / 32];
+          if constexpr (FMT == 2 && CH == 4) x.v[4 * sub + j][0] = *reinterpret_cast<const uint16_t*>(vp + at + j * rowb);
+          else load_words<TL::kVWords>(vp + at + j * rowb, x.v[4 * sub + j]);
         }
+        if constexpr (FMT != 0) {
+          const uint8_t* sp = a.vs + prow[sub] * nb;
+          if constexpr (EX && DP == 64) {
+            uint32_t w[2];
+            load_words<2>(sp + uint32_t(fresh(8 * g)), w);
+            x.vs[4 * sub] = w[0], x.vs[4 * sub + 1] = w[0] >> 16, x.vs[4 * sub + 2] = w[1], x.vs[4 * sub + 3] = w[1] >> 16;
+          } else if constexpr (EX && DP == 128) {
+            load_words<4>(sp + uint32_t(fresh(16 * g)), x.vs + 4 * sub);
+          } else if constexpr (EX) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) load_words<1>(sp + uint32_t(fresh(32 * g + 4 * (n16 >> 3))) + 8 * j, x.vs + 4 * sub + j);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x.vs[4 * sub + j] = uint32_t(sp[(4 * g + j) * nb + uint32_t(n16 * CH < D ? n16 * CH : 0) / 32]) << v_shift;
+          }
+        }
+      }
+    };
+    // One tile ahead: the next tile's K is asked for as soon as this one's is
+    // used up, its V at this one's end.  (The last tile asks for itself again:
+    // a branch here would have the next wait drain every load.)
+    int64_t prow[2];
+    if (t < tile_b) {
+      load_pages(t);
+      places(t, prow);
+      load_k(prow);
+      load_v(prow);
+    }
+    // (the queries are here before the loop: in it, a wait for them would be one for every load)
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int j = 0; j < TL::kSteps; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) asm volatile("" : "+v"(qf[r][j][e]));
+    // A wave gives way as it gets on: of those that wait for memory the oldest
+    // would go first, and the youngest start when the others are done.
+    const int third = max(1, (tile_b - t + 3 * kWaves - 1) / (3 * kWaves)) * kWaves;  // tiles of its first third
+    const int q1 = t + third, q2 = q1 + third;
+    __builtin_amdgcn_s_setprio(2);
+    for (; t < tile_b; t += kWaves) {
+      const int tok0 = t * kTile;
+      if (t == q1) __builtin_amdgcn_s_setprio(1);
+      if (t == q2) __builtin_amdgcn_s_setprio(0);
+      if (t + kWaves < tile_b) {
+        if (t + kWaves - page_at >= 32 * kWaves) load_pages(t + kWaves);
+        places(t + kWaves, prow);
       }
       // scores: K (16 tokens x channels) times the rows' queries
       f32x4 sc[R][2];
@@ -307,36 +540,20 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
         for (int j = 0; j < TL::kSteps; ++j) {
           constexpr int per = TL::kChunk / 8;
           uint32_t kw[4];
-          decode_words<FMT, T>(x.k[sub], j, FMT ? scale_of(x.ks[sub][j / per]) : 1.0f, kw);
+          const int i = j / per;
+          decode_words<FMT, T>(x.k[sub], j, FMT ? scale_at(x.ks[sub][i * TL::kChunk / 32], 8 * (i * TL::kChunk / 8 % 4) + k_shift) : 1.0f, kw);
 #pragma unroll
           for (int r = 0; r < R; ++r)
             sc[r][sub] = T::mfma16(u32x4{kw[0], kw[1], kw[2], kw[3]}, u32x4{qf[r][j][0], qf[r][j][1], qf[r][j][2], qf[r][j][3]}, sc[r][sub]);
         }
       }
-      // V: pairs of tokens per channel from pairs of channels per token
-      uint32_t vt[8][CH / 2];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float s = FMT ? scale_of(x.vs[j]) : 1.0f;
-        if constexpr (CH == 4) {
-          if constexpr (FMT == 0) vt[j][0] = x.v[j][0], vt[j][1] = x.v[j][1];
-          else if constexpr (FMT == 1) vt[j][0] = T::template e4m3<false>(x.v[j][0], s), vt[j][1] = T::template e4m3<true>(x.v[j][0], s);
-          else vt[j][0] = T::template e2m1<0>(x.v[j][0], s), vt[j][1] = T::template e2m1<1>(x.v[j][0], s);
-        } else {
-#pragma unroll
-          for (int i = 0; i < CH / 8; ++i) {
-            uint32_t w[4];
-            decode_words<FMT, T>(x.v[j], i, s, w);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) vt[j][4 * i + e] = w[e];
-          }
-        }
-      }
+      load_k(prow);
+      __builtin_amdgcn_sched_barrier(0);
       const bool edge = tok0 + kTile > hi_min || tok0 < lo_max;
       if (edge) {
         // What a row does not see has no weight; and values that are not
-        // finite are left out, since 0 times them is not 0: not_finite_value
-        // gives them to the rows that see them.
+        // finite are left out, since 0 times them is not 0: the rows that see
+        // them get them below.
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -347,13 +564,10 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
               if (tok >= hi[r] || tok < lo[r]) sc[r][sub][i] = -INFINITY;
             }
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-          for (int e = 0; e < CH / 2; ++e) {
-            const uint32_t fm = finite_mask<T>(vt[j][e]);
-            odd |= fm != 0xffffffffu && tok0 + 16 * (j / 4) + 4 * g + j % 4 < hi_max;
-            vt[j][e] &= fm;
-          }
+        for (int j = 0; j < 8; ++j) {
+          const bool found = drop_not_finite<FMT, T, TL::kVWords>(x.v[j], x.vs[j], v_shift);
+          odd |= found && tok0 + 16 * (j / 4) + 4 * g + j % 4 < hi_max;
+        }
       }
       // softmax: the running maximum moves only when a score passes it by 8 powers of two
       uint32_t pw[R][4];
@@ -387,36 +601,26 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
 #pragma unroll
         for (int i = 0; i < 4; ++i) pw[r][i] = T::pack(sc[r][i / 2][2 * (i % 2)], sc[r][i / 2][2 * (i % 2) + 1]);
       }
-      // V^T (16 of a lane row's channels x 32 tokens) times the weights
+      // V^T (16 of a lane row's channels x 32 tokens) times the weights: pairs
+      // of tokens per channel from the tokens' pairs of channels
 #pragma unroll
-      for (int c = 0; c < CH; ++c) {
-        u32x4 w;
+      for (int cp = 0; cp < CH / 2; ++cp) {
+        uint32_t vt[8];
 #pragma unroll
-        for (int jj = 0; jj < 4; ++jj)
-          w[jj] = __builtin_amdgcn_perm(vt[2 * jj + 1][c / 2], vt[2 * jj][c / 2], c % 2 ? 0x07060302u : 0x05040100u);
+        for (int j = 0; j < 8; ++j) vt[j] = decode_pair<FMT, T>(x.v[j], cp, FMT ? scale_at(x.vs[j], v_shift) : 1.0f);
 #pragma unroll
-        for (int r = 0; r < R; ++r) o[r][c] = T::mfma16(w, u32x4{pw[r][0], pw[r][1], pw[r][2], pw[r][3]}, o[r][c]);
-      }
-    }
-    if (__builtin_expect(__ballot(odd) != 0, 0)) {
-      for (int t = tile_a + wave; t < tile_b; t += kWaves) {
-        const int tok0 = t * kTile;
-        if (!(tok0 + kTile > hi_min || tok0 < lo_max)) continue;
-        for (int tok = max(tok0, lo_min); tok < min(tok0 + kTile, hi_max); ++tok) {
-          const int64_t row = cached_row(a, table, h, tok);
-          if (row < 0) continue;
-          const int c0 = fresh(4 * g * CH);
+        for (int e = 0; e < 2; ++e) {
+          u32x4 w;
 #pragma unroll
-          for (int r = 0; r < R; ++r) {
-            const bool sees = tok < hi[r] && tok >= lo[r];
+          for (int jj = 0; jj < 4; ++jj) w[jj] = __builtin_amdgcn_perm(vt[2 * jj + 1], vt[2 * jj], e ? 0x07060302u : 0x05040100u);
 #pragma unroll
-            for (int c = 0; c < CH; ++c)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) o[r][c][e] += not_finite_value<FMT, T>(a, row, c0 + e * CH + c, sees);
-          }
+          for (int r = 0; r < R; ++r) o[r][2 * cp + e] = T::mfma16(w, u32x4{pw[r][0], pw[r][1], pw[r][2], pw[r][3]}, o[r][2 * cp + e]);
         }
       }
+      load_v(prow);
+      __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_s_setprio(3);
     // this lane's tokens of the sums: over the four lanes of a row
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -426,102 +630,98 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(const AttnArgs a
       if (g == 0) s_m[wave][16 * r + n16] = m[r], s_l[wave][16 * r + n16] = l[r];
     }
     __syncthreads();
+    if (__builtin_expect(odd, 0)) s_odd = 1;
 
     // The waves' rows joined: each at the common maximum, summed in wave order.
-    const bool whole = ua == 0 && ub == sw.cnt;
-    const int slot = 2 * wg + (ua == 0 ? 1 : 0);
-    float* part = a.part + int64_t(slot) * (MT * DP);
-    float* part_ml = a.part_ml + int64_t(slot) * (2 * MT);
+    const int slot = slot0 + task * parts + part;
+    float* to_part = a.part + int64_t(slot) * (MT * DP);
+    float* to_ml = a.part_ml + int64_t(slot) * (2 * MT);
+    auto give = [&](int row, int ch, f32x4 acc, float L) {
+      const int rr = r0 + row, i = rr / G, hh = rr - i * G;
+      const float inv = pos0 + i < 0 && L == 0.0f ? 0.0f : 1.0f / L;  // (no position: nothing was summed)
+      uint16_t* dst = a.out + (token_row0 + i) * a.out_stride + int64_t(h * G + hh) * D + ch;
+      *reinterpret_cast<u32x2*>(dst) = u32x2{T::pack(acc[0] * inv, acc[1] * inv), T::pack(acc[2] * inv, acc[3] * inv)};
+    };
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int row = 16 * r + n16;
       float M = s_m[0][row];
 #pragma unroll
       for (int w = 1; w < kWaves; ++w) M = fmaxf(M, s_m[w][row]);
-      const float f = m[r] == M ? 1.0f : exp2f(m[r] - M);
+      const float f = m[r] == M ? 1.0f : __builtin_amdgcn_exp2f(m[r] - M);
 #pragma unroll
       for (int half = 0; half < DP / CW; ++half) {
         if (DP == CW || (4 * g * CH) / CW == half) {
 #pragma unroll
           for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int c = 0; c < CH; ++c) s_o[wave][n16][(4 * g + i) * CH + c - half * CW] = o[r][c][i] * f;
+            for (int c = 0; c < CH; c += 4)
+              *reinterpret_cast<f32x4*>(&s_o[wave][n16][(4 * g + i) * CH + c - half * CW]) =
+                  f32x4{o[r][c][i] * f, o[r][c + 1][i] * f, o[r][c + 2][i] * f, o[r][c + 3][i] * f};
+        }
+        if (half == 0 && g == 0 && wave == kWaves - 1) {
+          float L = 0.0f;
+#pragma unroll
+          for (int w = 0; w < kWaves; ++w) L += s_l[w][row] * (s_m[w][row] == M ? 1.0f : __builtin_amdgcn_exp2f(s_m[w][row] - M));
+          s_sum[row] = L;
+          if (row < nrow && parts > 1) qtea_detail::store_coherent(to_ml + row, M), qtea_detail::store_coherent(to_ml + MT + row, L);
         }
         __syncthreads();
-        for (int e = tid; e < 16 * (CW / 4); e += kThreads) {
+        for (int e = tid; e < min(16, nrow - 16 * r) * (CW / 4); e += kRowThreads) {
           const int rw = e / (CW / 4), c4 = (e % (CW / 4)) * 4, row2 = 16 * r + rw, ch = half * CW + c4;
-          float M2 = s_m[0][row2];
+          if (ch >= D) continue;
+          f32x4 acc = *reinterpret_cast<const f32x4*>(&s_o[0][rw][c4]);
 #pragma unroll
-          for (int w = 1; w < kWaves; ++w) M2 = fmaxf(M2, s_m[w][row2]);
-          float L = 0;
-          f32x4 acc = {0, 0, 0, 0};
+          for (int w = 1; w < kWaves; ++w) acc += *reinterpret_cast<const f32x4*>(&s_o[w][rw][c4]);
+          if (__builtin_expect(s_odd, 0)) {
+            // values that are not finite, of the tokens this row sees
+            const int i = (r0 + row2) / G;
+            const int to = min(tile_b * kTile, max(0, pos0 + i + 1)), from = a.window > 0 ? max(0, pos0 + i + 1 - a.window) : 0;
+            for (int tok = max(tile_a * kTile, from); tok < to; ++tok) {
+              const int tok0 = tok & ~(kTile - 1);
+              const int64_t at = tok0 + kTile > hi_min || tok0 < lo_max ? cached_row(a, table, h, tok) : -1;
+              if (at < 0) continue;  // (of another tile: taken with the rest)
 #pragma unroll
-          for (int w = 0; w < kWaves; ++w) {
-            const float mw = s_m[w][row2];
-            L += s_l[w][row2] * (mw == M2 ? 1.0f : exp2f(mw - M2));
-            acc += *reinterpret_cast<const f32x4*>(&s_o[w][rw][c4]);
-          }
-          if (row2 < nrow && ch < D) {
-            if (whole) {
-              const int rr = r0 + row2, i = rr / G, hh = rr - i * G;
-              // (no position: nothing was summed)
-              const float inv = pos0 + i < 0 && L == 0.0f ? 0.0f : 1.0f / L;
-              uint32_t w2[2] = {T::pack(acc[0] * inv, acc[1] * inv), T::pack(acc[2] * inv, acc[3] * inv)};
-              uint16_t* dst = a.out + (token_row0 + i) * a.out_stride + int64_t(h * G + hh) * D + ch;
-              *reinterpret_cast<u32x2*>(dst) = u32x2{w2[0], w2[1]};
-            } else {
-#pragma unroll
-              for (int i = 0; i < 4; ++i) qtea_detail::store_coherent(part + row2 * DP + ch + i, acc[i]);
-              if (ch == 0) {
-                qtea_detail::store_coherent(part_ml + row2, M2);
-                qtea_detail::store_coherent(part_ml + MT + row2, L);
-              }
+              for (int e2 = 0; e2 < 4; ++e2) acc[e2] += not_finite_value<FMT, T>(a, at, ch + e2);
             }
           }
-        }
-        __syncthreads();
-      }
-    }
-    if (!whole) {
-      // The last of the task's workgroups to arrive sums their parts, in run order.
-      const int first_u = u - ua, ga = run_owner(first_u, W, NG), gb = run_owner(first_u + sw.cnt - 1, W, NG);
-      __builtin_amdgcn_s_waitcnt(0);  // the part is complete before its arrival is counted
-      __syncthreads();
-      if (tid == 0) {
-        const uint32_t before = __hip_atomic_fetch_add(a.counters + ga, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        const bool last = before == uint32_t(gb - ga);
-        if (last) __hip_atomic_store(a.counters + ga, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        s_last = last;
-      }
-      __syncthreads();
-      if (s_last) {
-        for (int e = tid; e < nrow * (DP / 4); e += kThreads) {
-          const int row2 = e / (DP / 4), ch = (e % (DP / 4)) * 4;
-          if (ch >= D) continue;
-          float M2 = -INFINITY, L = 0;
-          f32x4 acc = {0, 0, 0, 0};
-          for (int w = ga; w <= gb; ++w) {
-            const int64_t sl = 2 * w + (w == ga ? 1 : 0);
-            const float mw = qtea_detail::load_coherent(a.part_ml + sl * (2 * MT) + row2);
-            const float lw = qtea_detail::load_coherent(a.part_ml + sl * (2 * MT) + MT + row2);
-            f32x4 ow;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) ow[i] = qtea_detail::load_coherent(a.part + sl * (MT * DP) + row2 * DP + ch + i);
-            const float now = fmaxf(M2, mw);
-            const float fa = M2 == now ? 1.0f : exp2f(M2 - now), fb = mw == now ? 1.0f : exp2f(mw - now);
-            M2 = now;
-            L = L * fa + lw * fb;
-            acc = acc * fa + ow * fb;
+          if (parts == 1) {
+            give(row2, ch, acc, s_sum[row2]);
+          } else {
+            store_coherent2(to_part + row2 * DP + ch, acc[0], acc[1]);
+            store_coherent2(to_part + row2 * DP + ch + 2, acc[2], acc[3]);
           }
-          const int rr = r0 + row2, i = rr / G, hh = rr - i * G;
-          const float inv = pos0 + i < 0 && L == 0.0f ? 0.0f : 1.0f / L;
-          uint16_t* dst = a.out + (token_row0 + i) * a.out_stride + int64_t(h * G + hh) * D + ch;
-          *reinterpret_cast<u32x2*>(dst) = u32x2{T::pack(acc[0] * inv, acc[1] * inv), T::pack(acc[2] * inv, acc[3] * inv)};
         }
         __syncthreads();
       }
     }
-    u += ub - ua;
+    if (parts > 1) {
+      // The last of the task's workgroups to arrive joins their parts, in
+      // order; of more than kJoin parts, first the last of every kJoin joins
+      // those, into the place of their first (with maxima and sums of their
+      // own: other threads may still read the parts').
+      float* joined_ml = a.part_ml + int64_t(a.max_slots) * (2 * MT);
+      const bool tree = parts > kJoin;
+      const int first = slot - part, mine0 = first + (tree ? part / kJoin * kJoin : 0), n_mine = tree ? min(kJoin, first + parts - mine0) : parts;
+      if (last_to_arrive(a.counters + mine0, n_mine, &s_last)) {
+        if (tree) {
+          join_parts<DP, MT, kRowThreads>(a, a.part_ml, mine0, 1, n_mine, nrow, &s_o[0][0][0], [&](int row, int ch, const Joined& j) {
+            float* at = a.part + int64_t(mine0) * (MT * DP) + row * DP + ch;
+            store_coherent2(at, j.acc[0], j.acc[1]);
+            store_coherent2(at + 2, j.acc[2], j.acc[3]);
+            if (ch == 0) {
+              float* ml = joined_ml + int64_t(mine0) * (2 * MT) + row;
+              qtea_detail::store_coherent(ml, j.M), qtea_detail::store_coherent(ml + MT, j.L);
+            }
+          });
+          if (last_to_arrive(a.counters + a.max_slots + first, (parts + kJoin - 1) / kJoin, &s_last))
+            join_parts<DP, MT, kRowThreads>(a, joined_ml, first, kJoin, (parts + kJoin - 1) / kJoin, nrow, &s_o[0][0][0], [&](int row, int ch, const Joined& j) { give(row, ch, j.acc, j.L); });
+        } else {
+          join_parts<DP, MT, kRowThreads>(a, a.part_ml, first, 1, parts, nrow, &s_o[0][0][0], [&](int row, int ch, const Joined& j) { give(row, ch, j.acc, j.L); });
+        }
+      }
+      __syncthreads();
+    }
   }
 }
 
@@ -802,12 +1002,12 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attn_tile_kernel(
       for (int tok = max(tok0, lo_min); tok < min(tok0 + KT, hi_max); ++tok) {
         const int64_t row = cached_row(a, table, h, tok);
         if (row < 0) continue;
-        const bool sees = tok < hi && tok >= lo;
+        if (tok >= hi || tok < lo) continue;
         const int c0 = fresh(4 * half);
 #pragma unroll
         for (int c = 0; c < CB; ++c)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) o[c][i] += not_finite_value<FMT, T>(a, row, c0 + 32 * c + 8 * (i >> 2) + (i & 3), sees);
+          for (int i = 0; i < 16; ++i) o[c][i] += not_finite_value<FMT, T>(a, row, c0 + 32 * c + 8 * (i >> 2) + (i & 3));
       }
     }
   }
@@ -837,48 +1037,22 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attn_tile_kernel(
 #pragma unroll
     for (int c = 0; c < CB; ++c)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
+      for (int i = 0; i < 16; i += 2) {
         const int ch = 32 * c + 8 * (i >> 2) + 4 * half + (i & 3);
-        if (ch < D) qtea_detail::store_coherent(mine + ch, o[c][i]);
+        if (ch < D) store_coherent2(mine + ch, o[c][i], o[c][i + 1]);
       }
     if (half == 0) {
       qtea_detail::store_coherent(ml, m);
       qtea_detail::store_coherent(ml + kTaskRows, l);
     }
   }
-  __builtin_amdgcn_s_waitcnt(0);  // the part is complete before its arrival is counted
-  __syncthreads();
-  if (tid == 0) {
-    const uint32_t before = __hip_atomic_fetch_add(a.counters + id, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const bool last = before == uint32_t(used - 1);
-    if (last) __hip_atomic_store(a.counters + id, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    s_last = last;
-  }
-  __syncthreads();
-  if (!s_last) return;
-  for (int e = tid; e < nrow * (DP / 4); e += kThreads) {
-    const int row = e / (DP / 4), ch = (e % (DP / 4)) * 4;
-    if (ch >= D) continue;
-    float M = -INFINITY, L = 0.0f;
-    f32x4 acc = {0, 0, 0, 0};
-    for (int w = 0; w < used; ++w) {
-      const float* pm = a.part_ml + (slot0 + w) * (2 * kTaskRows) + row;
-      const float* po = a.part + (slot0 + w) * (kTaskRows * DP) + row * DP + ch;
-      const float mw = qtea_detail::load_coherent(pm), lw = qtea_detail::load_coherent(pm + kTaskRows);
-      f32x4 ow;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) ow[i] = qtea_detail::load_coherent(po + i);
-      const float now = fmaxf(M, mw);
-      const float fa = M == now ? 1.0f : exp2f(M - now), fb = mw == now ? 1.0f : exp2f(mw - now);
-      M = now;
-      L = L * fa + lw * fb;
-      acc = acc * fa + ow * fb;
-    }
+  if (!last_to_arrive(a.counters + id, used, &s_last)) return;
+  join_parts<DP, kTaskRows, kThreads>(a, a.part_ml, slot0, 1, used, nrow, reinterpret_cast<float*>(&s_k[0][0]), [&](int row, int ch, const Joined& j) {
     const int r = r0 + row, i = r / G;
-    const float inv = pos0 + i < 0 && L == 0.0f ? 0.0f : 1.0f / L;
+    const float inv = pos0 + i < 0 && j.L == 0.0f ? 0.0f : 1.0f / j.L;
     uint16_t* to = a.out + (int64_t(q.first) + i) * a.out_stride + int64_t(h * G + (r - i * G)) * D + ch;
-    *reinterpret_cast<u32x2*>(to) = u32x2{T::pack(acc[0] * inv, acc[1] * inv), T::pack(acc[2] * inv, acc[3] * inv)};
-  }
+    *reinterpret_cast<u32x2*>(to) = u32x2{T::pack(j.acc[0] * inv, j.acc[1] * inv), T::pack(j.acc[2] * inv, j.acc[3] * inv)};
+  });
 }
 
 int device_cus() {
@@ -889,21 +1063,24 @@ int device_cus() {
   });
 }
 
-// The workspace: counters, the parts' maxima and sums, the parts; for the
-// grid of the one kernel with two parts a workgroup, and for as many
-// workgroups of the other, one part each.
+// The workspace: counters, the parts' maxima and sums, the parts.  The kernel
+// for few rows has a slot for every chunk of a split task, of which there are
+// no more than workgroups where all chunks fit them, and else less than
+// 2 / 1.5 of that (a split task's last chunk is the only one that may be short).
 constexpr int kRowsMax = 32;
+constexpr int kSlotsPerCu = 5;
 struct WsLayout {
   int64_t ml, part, bytes;
 };
 int padded_dim(int dim) { return dim <= 64 ? 64 : (dim <= 128 ? 128 : 256); }
 WsLayout ws_layout(int dim, int cus) {
-  const int64_t grid = int64_t(cus) * kWgPerCu;
-  static_assert(kTaskRows >= 2 * kRowsMax, "the workspace holds either kernel's parts");
+  // (rows of the other kernel's parts, one a workgroup, hold all of these)
+  static_assert(kWgPerCu * kTaskRows >= 2 * kSlotsPerCu * 16 && kWgPerCu * kTaskRows >= 4 * kRowsMax, "slots of either kernel, twice for the maxima and sums");
+  const int64_t rows = int64_t(cus) * kWgPerCu * kTaskRows;
   WsLayout w;
-  w.ml = (4 * grid + 255) / 256 * 256;
-  w.part = w.ml + grid * 2 * kTaskRows * 4;
-  w.bytes = w.part + grid * kTaskRows * padded_dim(dim) * 4;
+  w.ml = (2 * 4 * int64_t(cus) * kSlotsPerCu + 255) / 256 * 256;  // (a counter per slot for each of two levels)
+  w.part = w.ml + rows * 2 * 4;
+  w.bytes = w.part + rows * padded_dim(dim) * 4;
   return w;
 }
 
@@ -952,6 +1129,7 @@ int qtea_paged_attention(const qtea_kv_cache* cache, const qtea_kv_batch* batch,
   a.b = kernel_batch(batch);
   a.heads = H, a.group = G, a.dim = D, a.page_shift = log2_of(cache->page_size), a.n_pages = int32_t(cache->n_pages), a.window = window;
   a.scale = scale * 1.44269504088896341f;
+  a.max_slots = cus * kSlotsPerCu;
   char* ws = static_cast<char*>(workspace);
   a.counters = reinterpret_cast<uint32_t*>(ws);
   a.part_ml = reinterpret_cast<float*>(ws + wl.ml);
@@ -970,13 +1148,20 @@ int qtea_paged_attention(const qtea_kv_cache* cache, const qtea_kv_batch* batch,
       hipLaunchKernelGGL((attn_tile_kernel<DP, FMT, T>), dim3(uint32_t(tasks * H * parts)), block, 0, st, a, parts);
       return;
     }
+    auto rows_launch = [&](auto r) {
+      constexpr int R = decltype(r)::value;
+      if (R == 2) a.max_slots = 2 * cus;
+      const dim3 wgs(cus * rows_per_cu(DP, FMT, R)), threads(kRowThreads);
+      if (D == DP) hipLaunchKernelGGL((attn_rows_kernel<DP, FMT, T, R, true>), wgs, threads, 0, st, a);
+      else hipLaunchKernelGGL((attn_rows_kernel<DP, FMT, T, R, false>), wgs, threads, 0, st, a);
+    };
     if constexpr (DP <= 128) {
       if (two) {
-        hipLaunchKernelGGL((attn_rows_kernel<DP, FMT, T, 2>), dim3(uint32_t(grid)), block, 0, st, a);
+        rows_launch(std::integral_constant<int, 2>());
         return;
       }
     }
-    hipLaunchKernelGGL((attn_rows_kernel<DP, FMT, T, 1>), dim3(uint32_t(grid)), block, 0, st, a);
+    rows_launch(std::integral_constant<int, 1>());
   };
   auto with_type = [&](auto dp, auto fmt) {
     if (type == QTEA_F16) launch(dp, fmt, F16());
