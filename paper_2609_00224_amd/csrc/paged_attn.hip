@@ -299,7 +299,7 @@ constexpr int lds_width(int DP) { return DP < 128 ? DP : 128; }  // channels joi
 constexpr float kMinUnits = 2.0f;  // of a chunk: what joining two costs
 // Workgroups per CU, each of one wave per SIMD: as many as have the registers
 // for a tile on the way beside their sums.
-constexpr int rows_per_cu(int DP, int FMT, int R) { return DP == 256 || R == 2 ? 1 : (FMT == 0 && DP == 128 ? 2 : 3); }
+constexpr int rows_per_cu(int DP, int FMT, int R) { return R * DP >= 256 ? 1 : (FMT == 0 && R * DP == 128 || R == 2 ? 2 : 3); }
 
 // EX: the heads have DP channels; else they have fewer, and what lies past
 // them is read from the first channels instead (queries are 0 there, and sums
@@ -573,6 +573,10 @@ __global__ __launch_bounds__(kRowThreads, rows_per_cu(DP, FMT, R)) void attn_row
       uint32_t pw[R][4];
 #pragma unroll
       for (int r = 0; r < R; ++r) {
+        if (r > 0 && 16 * r >= nrow) {  // (no such rows)
+          pw[r][0] = pw[r][1] = pw[r][2] = pw[r][3] = 0;
+          continue;
+        }
         float top = -INFINITY;
 #pragma unroll
         for (int sub = 0; sub < 2; ++sub)
@@ -1067,19 +1071,18 @@ int device_cus() {
 // for few rows has a slot for every chunk of a split task, of which there are
 // no more than workgroups where all chunks fit them, and else less than
 // 2 / 1.5 of that (a split task's last chunk is the only one that may be short).
-constexpr int kRowsMax = 32;
+constexpr int kRowsMax = 64;
 constexpr int kSlotsPerCu = 5;
 struct WsLayout {
   int64_t ml, part, bytes;
 };
 int padded_dim(int dim) { return dim <= 64 ? 64 : (dim <= 128 ? 128 : 256); }
 WsLayout ws_layout(int dim, int cus) {
-  // (rows of the other kernel's parts, one a workgroup, hold all of these)
-  static_assert(kWgPerCu * kTaskRows >= 2 * kSlotsPerCu * 16 && kWgPerCu * kTaskRows >= 4 * kRowsMax, "slots of either kernel, twice for the maxima and sums");
-  const int64_t rows = int64_t(cus) * kWgPerCu * kTaskRows;
+  static_assert(kSlotsPerCu * kRowsMax >= kWgPerCu * kTaskRows, "the other kernel's parts, one a workgroup");
+  const int64_t rows = int64_t(cus) * kSlotsPerCu * kRowsMax;
   WsLayout w;
-  w.ml = (2 * 4 * int64_t(cus) * kSlotsPerCu + 255) / 256 * 256;  // (a counter per slot for each of two levels)
-  w.part = w.ml + rows * 2 * 4;
+  w.ml = (2 * 4 * int64_t(cus) * kSlotsPerCu + 255) / 256 * 256;  // counters, maxima and sums: of two levels
+  w.part = w.ml + rows * 2 * 2 * 4;
   w.bytes = w.part + rows * padded_dim(dim) * 4;
   return w;
 }
@@ -1136,8 +1139,11 @@ int qtea_paged_attention(const qtea_kv_cache* cache, const qtea_kv_batch* batch,
   a.part = reinterpret_cast<float*>(ws + wl.part);
   const dim3 block(kThreads);
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  // The kernel by a sequence's rows on average (a call's lengths are only known on the device).
-  const bool many = rows > int64_t(kRowsMax) * batch->n_seq, two = D <= 128 && rows > int64_t(16) * batch->n_seq;
+  // The kernel by a sequence's rows on average (a call's lengths are only
+  // known on the device; with more than a token each, some have more).
+  const int64_t likely = batch->n_tokens > batch->n_seq ? rows + rows / 3 : rows;
+  const int halves = likely <= int64_t(16) * batch->n_seq ? 1 : (likely <= int64_t(32) * batch->n_seq || D > 128 ? 2 : 4);
+  const bool many = rows > int64_t(D > 128 ? 32 : 64) * batch->n_seq;
   const int64_t tasks = rows / kTaskRows + batch->n_seq, grid = int64_t(cus) * kWgPerCu;  // (tasks per head, at most)
   const int parts = int(std::max<int64_t>(1, std::min<int64_t>(grid / (tasks * H), kMaxParts)));
   if (many && tasks * H * parts > INT32_MAX) return QTEA_ERR_INVALID_ARG;
@@ -1150,18 +1156,13 @@ int qtea_paged_attention(const qtea_kv_cache* cache, const qtea_kv_batch* batch,
     }
     auto rows_launch = [&](auto r) {
       constexpr int R = decltype(r)::value;
-      if (R == 2) a.max_slots = 2 * cus;
       const dim3 wgs(cus * rows_per_cu(DP, FMT, R)), threads(kRowThreads);
       if (D == DP) hipLaunchKernelGGL((attn_rows_kernel<DP, FMT, T, R, true>), wgs, threads, 0, st, a);
       else hipLaunchKernelGGL((attn_rows_kernel<DP, FMT, T, R, false>), wgs, threads, 0, st, a);
     };
-    if constexpr (DP <= 128) {
-      if (two) {
-        rows_launch(std::integral_constant<int, 2>());
-        return;
-      }
-    }
-    rows_launch(std::integral_constant<int, 1>());
+    if (halves == 1) rows_launch(std::integral_constant<int, 1>());
+    else if (halves == 2) rows_launch(std::integral_constant<int, 2>());
+    else if constexpr (DP <= 128) rows_launch(std::integral_constant<int, 4>());
   };
   auto with_type = [&](auto dp, auto fmt) {
     if (type == QTEA_F16) launch(dp, fmt, F16());
