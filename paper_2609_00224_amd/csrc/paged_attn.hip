@@ -242,6 +242,7 @@ __device__ __forceinline__ bool last_to_arrive(uint32_t* counter, int n, int* s_
 }
 
 constexpr int kJoin = 12;  // parts joined at once
+constexpr int kCounterWords = 32;  // a line a counter: arrivals at one line are served one after another
 
 // Joins the parts of a task's rows in part order, by the whole workgroup: four
 // channels a thread, and with few rows the parts dealt to groups of threads,
@@ -707,7 +708,7 @@ __global__ __launch_bounds__(kRowThreads, rows_per_cu(DP, FMT, R)) void attn_row
       float* joined_ml = a.part_ml + int64_t(a.max_slots) * (2 * MT);
       const bool tree = parts > kJoin;
       const int first = slot - part, mine0 = first + (tree ? part / kJoin * kJoin : 0), n_mine = tree ? min(kJoin, first + parts - mine0) : parts;
-      if (last_to_arrive(a.counters + mine0, n_mine, &s_last)) {
+      if (last_to_arrive(a.counters + mine0 * kCounterWords, n_mine, &s_last)) {
         if (tree) {
           join_parts<DP, MT, kRowThreads>(a, a.part_ml, mine0, 1, n_mine, nrow, &s_o[0][0][0], [&](int row, int ch, const Joined& j) {
             float* at = a.part + int64_t(mine0) * (MT * DP) + row * DP + ch;
@@ -718,7 +719,7 @@ __global__ __launch_bounds__(kRowThreads, rows_per_cu(DP, FMT, R)) void attn_row
               qtea_detail::store_coherent(ml, j.M), qtea_detail::store_coherent(ml + MT, j.L);
             }
           });
-          if (last_to_arrive(a.counters + a.max_slots + first, (parts + kJoin - 1) / kJoin, &s_last))
+          if (last_to_arrive(a.counters + (a.max_slots + first) * kCounterWords, (parts + kJoin - 1) / kJoin, &s_last))
             join_parts<DP, MT, kRowThreads>(a, joined_ml, first, kJoin, (parts + kJoin - 1) / kJoin, nrow, &s_o[0][0][0], [&](int row, int ch, const Joined& j) { give(row, ch, j.acc, j.L); });
         } else {
           join_parts<DP, MT, kRowThreads>(a, a.part_ml, first, 1, parts, nrow, &s_o[0][0][0], [&](int row, int ch, const Joined& j) { give(row, ch, j.acc, j.L); });
@@ -1050,7 +1051,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attn_tile_kernel(
       qtea_detail::store_coherent(ml + kTaskRows, l);
     }
   }
-  if (!last_to_arrive(a.counters + id, used, &s_last)) return;
+  if (!last_to_arrive(a.counters + id * kCounterWords, used, &s_last)) return;
   join_parts<DP, kTaskRows, kThreads>(a, a.part_ml, slot0, 1, used, nrow, reinterpret_cast<float*>(&s_k[0][0]), [&](int row, int ch, const Joined& j) {
     const int r = r0 + row, i = r / G;
     const float inv = pos0 + i < 0 && j.L == 0.0f ? 0.0f : 1.0f / j.L;
@@ -1081,7 +1082,7 @@ WsLayout ws_layout(int dim, int cus) {
   static_assert(kSlotsPerCu * kRowsMax >= kWgPerCu * kTaskRows, "the other kernel's parts, one a workgroup");
   const int64_t rows = int64_t(cus) * kSlotsPerCu * kRowsMax;
   WsLayout w;
-  w.ml = (2 * 4 * int64_t(cus) * kSlotsPerCu + 255) / 256 * 256;  // counters, maxima and sums: of two levels
+  w.ml = 2 * 4 * int64_t(cus) * kSlotsPerCu * kCounterWords;  // counters, maxima and sums: of two levels
   w.part = w.ml + rows * 2 * 2 * 4;
   w.bytes = w.part + rows * padded_dim(dim) * 4;
   return w;

@@ -19,9 +19,10 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxSlices = 64;      // a wave scans their sums
-constexpr int kMinSlice = 2048;     // vocabulary entries: 8 per thread
+constexpr int kBlock = 8 * kThreads;  // vocabulary entries of one step; slices are whole blocks
 constexpr int kTargetBlocks = 2048; // workgroups that keep HBM busy
-constexpr int64_t kCounterBytes = 256;
+constexpr int64_t kCounterBytes = 128;  // a line each: arrivals at one line are served one after another
+constexpr int64_t kSeqBytes = kCounterBytes + kMaxSlices * 16;
 
 struct VerifyArgs {
   const char* target;
@@ -33,8 +34,8 @@ struct VerifyArgs {
   const float* u_sample;
   int32_t* n_accepted;
   int32_t* out_tokens;
-  uint32_t* counters;  // [n_seq]
-  uint64_t* sums;      // [n_seq][slices][2]: of max(P - Q, 0), of P
+  char* counters;  // [n_seq], kCounterBytes apart
+  uint64_t* sums;  // [n_seq][kMaxSlices][2]: of max(P - Q, 0), of P
   int32_t vocab, n_seq, n_rows, n_drafts, max_draft, slices, slice;
 };
 
@@ -45,14 +46,23 @@ __device__ __forceinline__ float prob(const char* row, int64_t v) {
   return __uint_as_float(uint32_t(reinterpret_cast<const uint16_t*>(row)[v]) << 16);
 }
 
-// A probability in whole units of 2^-38 (NaN: 0).
-__device__ __forceinline__ uint64_t fixed(float p) {
-  const float c = p > 0.0f ? fminf(p, 1.0f) : 0.0f;
-  // its 24 significant bits, shifted: exact, and truncated below the unit
-  const uint32_t b = __float_as_uint(c);
-  const int sh = int(b >> 23) - 150 + 38;  // (subnormal values are far below the unit)
-  const uint64_t m = (b & 0x7fffffu) | 0x800000u;
-  return sh >= 0 ? m << sh : (sh > -24 ? m >> -sh : 0);
+// A probability in whole units of 2^-38, floor(2^38 p) (p limited to [0, 1],
+// NaN: 0): its units of 2^-19, and what is left of it (exact) in units of 2^-38.
+struct Fixed {
+  uint32_t hi, lo;
+  __device__ __forceinline__ uint64_t whole() const { return (uint64_t(hi) << 19) + lo; }
+};
+__device__ __forceinline__ Fixed fixed(float p) {
+  const float c = __builtin_amdgcn_fmed3f(p > 0.0f ? p : 0.0f, 0.0f, 1.0f) * 0x1p19f;
+  Fixed f;
+  f.hi = uint32_t(c);
+  f.lo = uint32_t((c - float(f.hi)) * 0x1p19f);
+  return f;
+}
+// max(p - q, 0)
+__device__ __forceinline__ uint64_t over(Fixed p, Fixed q) {
+  const int64_t d = (int64_t(int32_t(p.hi) - int32_t(q.hi)) << 19) + (int32_t(p.lo) - int32_t(q.lo));
+  return d > 0 ? uint64_t(d) : 0;
 }
 
 // A random number in units of 2^-24.
@@ -61,50 +71,35 @@ __device__ __forceinline__ uint64_t unit24(float u) { return u > 0.0f ? min(uint
 __device__ __forceinline__ uint64_t load64(const uint64_t* p) {
   return __hip_atomic_load(const_cast<uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-__device__ __forceinline__ uint64_t shfl64(uint64_t x, int lane) {
-  return uint64_t(uint32_t(__shfl(int(uint32_t(x)), lane))) | uint64_t(uint32_t(__shfl(int(uint32_t(x >> 32)), lane))) << 32;
+__device__ __forceinline__ uint64_t readlane64(uint64_t x, int lane) {
+  return uint64_t(uint32_t(__builtin_amdgcn_readlane(int(uint32_t(x)), lane))) | uint64_t(uint32_t(__builtin_amdgcn_readlane(int(uint32_t(x >> 32)), lane))) << 32;
 }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t dpp64(uint64_t x) {
+  const uint32_t lo = uint32_t(__builtin_amdgcn_update_dpp(0, int(uint32_t(x)), CTRL, ROWS, 0xf, false));
+  const uint32_t hi = uint32_t(__builtin_amdgcn_update_dpp(0, int(uint32_t(x >> 32)), CTRL, ROWS, 0xf, false));
+  return uint64_t(hi) << 32 | lo;
+}
+// Inclusive sum over the wave's lanes.
 __device__ __forceinline__ uint64_t wave_scan64(uint64_t x) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint64_t y = shfl64(x, max(lane - d, 0));
-    if (lane >= d) x += y;
-  }
+  x += dpp64<0x111, 0xf>(x);  // from 1, 2, 4, 8 lanes below in the row of 16
+  x += dpp64<0x112, 0xf>(x);
+  x += dpp64<0x114, 0xf>(x);
+  x += dpp64<0x118, 0xf>(x);
+  x += dpp64<0x142, 0xa>(x);  // a row's last lane to the next row
+  x += dpp64<0x143, 0xc>(x);  // lane 31 to the upper half
   return x;
-}
-
-// 8 weights' P and Q from vocabulary entry v on (0 past the end).
-template <int TYPE>
-__device__ __forceinline__ void load8(const char* row, int v, int end, bool wide, float (&x)[8]) {
-  constexpr int kSize = TYPE == QTEA_F32 ? 4 : 2;
-  if (wide && v + 8 <= end) {
-    if constexpr (TYPE == QTEA_F32) {
-      const f32x4 a = *reinterpret_cast<const f32x4*>(row + int64_t(v) * kSize), b = *reinterpret_cast<const f32x4*>(row + int64_t(v) * kSize + 16);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
-    } else {
-      const u32x4 a = *reinterpret_cast<const u32x4*>(row + int64_t(v) * kSize);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint16_t hw = uint16_t(a[i / 2] >> (16 * (i % 2)));
-        x[i] = TYPE == QTEA_F16 ? qtea_detail::h2f(hw) : __uint_as_float(uint32_t(hw) << 16);
-      }
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = v + i < end ? prob<TYPE>(row, v + i) : 0.0f;
-  }
 }
 
 template <int TYPE, bool DRAFT>
 __global__ __launch_bounds__(kThreads) void verify_kernel(const VerifyArgs a) {
-  __shared__ uint64_t s_sum[4][2], s_scan[4];
+  __shared__ uint64_t s_sum[4][2], s_scan[4], s_w[kBlock];
   __shared__ int s_last, s_token;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int s = blockIdx.x / a.slices, slice = blockIdx.x - s * a.slices;
   const int first = min(max(a.q_start[s], 0), a.n_rows), rows = min(max(a.q_start[s + 1], 0), a.n_rows) - first;
   int32_t* out = a.out_tokens + int64_t(s) * (a.max_draft + 1);
+  const uint64_t u_sample = unit24(a.u_sample[s]);
   if (rows <= 0) {
     if (slice == 0) {
       for (int i = tid; i <= a.max_draft; i += kThreads) out[i] = -1;
@@ -132,8 +127,8 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(const VerifyArgs a) {
       const int x = in ? a.tokens[d] : -1;
       if (x < 0 || x >= a.vocab) ok = false;
       else {
-        const uint64_t P = fixed(prob<TYPE>(a.target + (int64_t(first) + i) * a.target_stride, x));
-        const uint64_t Q = DRAFT ? fixed(prob<TYPE>(a.draft + int64_t(d) * a.draft_stride, x)) : uint64_t(1) << 38;
+        const uint64_t P = fixed(prob<TYPE>(a.target + (int64_t(first) + i) * a.target_stride, x)).whole();
+        const uint64_t Q = DRAFT ? fixed(prob<TYPE>(a.draft + int64_t(d) * a.draft_stride, x)).whole() : uint64_t(1) << 38;
         ok = unit24(a.u_accept[d]) * Q < P << 24;
       }
     }
@@ -150,37 +145,35 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(const VerifyArgs a) {
   const char* p_row = a.target + (int64_t(first) + acc) * a.target_stride;
   const char* q_row = has_q && DRAFT ? a.draft + int64_t(dr) * a.draft_stride : nullptr;
   const int x_one = has_q && !DRAFT ? a.tokens[dr] : -1;  // where a deterministic draft had its whole mass
-  const bool p_wide = (reinterpret_cast<uintptr_t>(p_row) & 15) == 0, q_wide = (reinterpret_cast<uintptr_t>(q_row) & 15) == 0;
-  const int v0 = slice * a.slice;
-
+  // W and P of entries v + 256 i (0 past the end), i < 8: every load on its way
+  // before the first is used, a wave's lanes on consecutive entries
   auto weights = [&](int v, int end, uint64_t (&w)[8], uint64_t (&p)[8]) {
-    float x[8];
-    load8<TYPE>(p_row, v, end, p_wide, x);
+    float x[8], y[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = p[i] = fixed(x[i]);
+    for (int i = 0; i < 8; ++i) x[i] = prob<TYPE>(p_row, min(v + kThreads * i, end - 1));
     if (DRAFT && q_row) {
-      load8<TYPE>(q_row, v, end, q_wide, x);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint64_t q = fixed(x[i]);
-        w[i] = p[i] > q ? p[i] - q : 0;
-      }
+      for (int i = 0; i < 8; ++i) y[i] = prob<TYPE>(q_row, min(v + kThreads * i, end - 1));
     }
-    if (!DRAFT) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) w[i] = v + i == x_one ? 0 : p[i];  // (P is at most 1)
+    for (int i = 0; i < 8; ++i) {
+      const bool in = v + kThreads * i < end;
+      const Fixed f = fixed(in ? x[i] : 0.0f);
+      w[i] = p[i] = f.whole();
+      if (DRAFT && q_row) w[i] = over(f, fixed(y[i]));
+      if (!DRAFT && v + kThreads * i == x_one) w[i] = 0;  // (P is at most 1)
     }
   };
 
+  const int v0 = slice * a.slice, v1 = min(v0 + a.slice, a.vocab);
   uint64_t sw = 0, sp = 0;
-  for (int v = v0 + 8 * tid; v < min(v0 + a.slice, a.vocab); v += 8 * kThreads) {
+  for (int v = v0; v < v1; v += kBlock) {
     uint64_t w[8], p[8];
-    weights(v, min(v0 + a.slice, a.vocab), w, p);
+    weights(v + tid, v1, w, p);
 #pragma unroll
     for (int i = 0; i < 8; ++i) sw += w[i], sp += p[i];
   }
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) sw += shfl64(sw, lane ^ d), sp += shfl64(sp, lane ^ d);
+  sw = readlane64(wave_scan64(sw), 63), sp = readlane64(wave_scan64(sp), 63);
   if (lane == 0) s_sum[wave][0] = sw, s_sum[wave][1] = sp;
   __syncthreads();
   uint64_t* sums = a.sums + int64_t(s) * (2 * kMaxSlices);
@@ -191,9 +184,10 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(const VerifyArgs a) {
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0);  // the sums are there before their arrival is counted
     asm volatile("" ::: "memory");
-    const uint32_t before = __hip_atomic_fetch_add(a.counters + s, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    uint32_t* counter = reinterpret_cast<uint32_t*>(a.counters + s * kCounterBytes);
+    const uint32_t before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     const bool last = before == uint32_t(a.slices - 1);
-    if (last) __hip_atomic_store(a.counters + s, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     s_last = last;
     s_token = -1;
   }
@@ -203,44 +197,41 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(const VerifyArgs a) {
   // the slice with the drawn position
   uint64_t tw = lane < a.slices ? load64(sums + 2 * lane) : 0, tp = lane < a.slices ? load64(sums + 2 * lane + 1) : 0;
   uint64_t cw = wave_scan64(tw), cp = wave_scan64(tp);
-  const bool from_p = shfl64(cw, 63) == 0;
+  const bool from_p = readlane64(cw, 63) == 0;
   if (from_p) cw = cp, tw = tp;
-  const uint64_t total = shfl64(cw, 63);
+  const uint64_t total = readlane64(cw, 63);
   if (total != 0) {
-    const uint64_t r = __umul64hi(total, unit24(a.u_sample[s]) << 40);  // floor(U total / 2^24)
+    const uint64_t r = __umul64hi(total, u_sample << 40);  // floor(U total / 2^24)
     const int at = __popcll(__ballot(cw <= r));  // (below 64: r < total)
-    uint64_t before = shfl64(cw, at) - shfl64(tw, at);
+    uint64_t before = readlane64(cw, at) - readlane64(tw, at);
     const int b0 = at * a.slice, b1 = min(b0 + a.slice, a.vocab);
-    for (int v = b0; v < b1; v += 8 * kThreads) {
+    for (int v = b0; v < b1 && before <= r; v += kBlock) {
+      // the block's weights by way of LDS: loaded 256 apart, summed 8 in a row
       uint64_t w[8], p[8];
-      const int mine = v + 8 * tid;
-      uint64_t sum = 0;
-      if (mine < b1) {
-        weights(mine, b1, w, p);
+      weights(v + tid, b1, w, p);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (from_p) w[i] = p[i];
-          sum += w[i];
-        }
-      }
+      for (int i = 0; i < 8; ++i) s_w[tid + kThreads * i] = from_p ? p[i] : w[i];
+      __syncthreads();
+      uint64_t sum = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += w[i] = s_w[8 * tid + i];
       const uint64_t incl = wave_scan64(sum);
       if (lane == 63) s_scan[wave] = incl;
       __syncthreads();
       uint64_t base = before;
       for (int i = 0; i < wave; ++i) base += s_scan[i];
       uint64_t c = base + incl - sum;
-      if (mine < b1 && c <= r && base + incl > r) {
+      if (c <= r && base + incl > r) {  // (one thread: the sums do not decrease)
         int k = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           c += w[i];
           k += c <= r ? 1 : 0;
         }
-        s_token = mine + k;
+        s_token = v + 8 * tid + k;
       }
       before += s_scan[0] + s_scan[1] + s_scan[2] + s_scan[3];
       __syncthreads();
-      if (before > r) break;
     }
   }
   const int token = s_token;
@@ -257,7 +248,7 @@ extern "C" {
 
 int qtea_verify_workspace_bytes(int n_seq, int64_t* out_bytes) {
   if (!out_bytes || n_seq < 1) return QTEA_ERR_INVALID_ARG;
-  *out_bytes = (4 * int64_t(n_seq) + kCounterBytes - 1) / kCounterBytes * kCounterBytes + int64_t(n_seq) * kMaxSlices * 16;
+  *out_bytes = int64_t(n_seq) * kSeqBytes;
   return QTEA_OK;
 }
 
@@ -282,14 +273,12 @@ int qtea_verify_draft(const void* target, const void* draft, int type, int64_t v
   a.target_stride = target_stride * size, a.draft_stride = draft_stride * size;
   a.tokens = tokens, a.q_start = q_start, a.u_accept = u_accept, a.u_sample = u_sample;
   a.n_accepted = n_accepted, a.out_tokens = out_tokens;
-  a.counters = static_cast<uint32_t*>(workspace);
-  a.sums = reinterpret_cast<uint64_t*>(static_cast<char*>(workspace) + (need - int64_t(n_seq) * kMaxSlices * 16));
+  a.counters = static_cast<char*>(workspace);
+  a.sums = reinterpret_cast<uint64_t*>(a.counters + int64_t(n_seq) * kCounterBytes);
   a.vocab = int32_t(vocab), a.n_seq = n_seq, a.n_rows = int32_t(n_rows), a.n_drafts = int32_t(n_drafts), a.max_draft = max_draft;
-  // Slices of at least kMinSlice entries, as many as fill the chip, at most
-  // kMaxSlices; a multiple of 8 entries each.
-  const int64_t want = std::max<int64_t>(1, kTargetBlocks / n_seq);
-  const int64_t parts = std::min<int64_t>({want, kMaxSlices, (vocab + kMinSlice - 1) / kMinSlice});
-  a.slice = int32_t(((vocab + parts - 1) / parts + 7) / 8 * 8);
+  // Slices of whole blocks: as many as fill the chip, at most kMaxSlices.
+  const int64_t want = std::min<int64_t>(std::max<int64_t>(1, kTargetBlocks / n_seq), kMaxSlices);
+  a.slice = int32_t((vocab + want * kBlock - 1) / (want * kBlock) * kBlock);
   a.slices = int32_t((vocab + a.slice - 1) / a.slice);
   if (int64_t(a.slices) * n_seq > INT32_MAX) return QTEA_ERR_INVALID_ARG;
   const dim3 grid(uint32_t(a.slices) * uint32_t(n_seq)), block(kThreads);

@@ -10,6 +10,10 @@ from __future__ import annotations
 
 import ctypes
 
+import torch
+
+import paper_2609_00224_amd as _q  # (its functions: this module is imported while it loads)
+
 QTEA_F16, QTEA_BF16, QTEA_F32 = 0, 1, 2
 QTEA_KV_BLOCK = 32
 KV_FORMATS = {"f16": 0, "bf16": 1, "e4m3": 2, "e2m1": 3}
@@ -48,25 +52,21 @@ def declare(lib):
         getattr(lib, name).restype = i
 
 
-def _package():
-    import paper_2609_00224_amd as q
-
-    return q
+_TYPES = {torch.float16: QTEA_F16, torch.bfloat16: QTEA_BF16, torch.float32: QTEA_F32}
+_I32, _F32 = torch.int32, torch.float32
 
 
 def _type(t, what):
-    import torch
-
-    got = {torch.float16: QTEA_F16, torch.bfloat16: QTEA_BF16, torch.float32: QTEA_F32}.get(t.dtype)
+    got = _TYPES.get(t.dtype)
     if got is None:
         raise ValueError(f"{what}: fp16, bf16 or fp32, got {t.dtype}")
     return got
 
 
-def _stream(stream):
-    import torch
-
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+def _stream(stream, device):
+    """The handle of `stream`, or of the device's current one (asked for
+    without making a torch.cuda.Stream of it, which takes 2.5 us)."""
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
 class KvCache:
@@ -76,8 +76,6 @@ class KvCache:
     [head_dim / 32] for the quantized formats."""
 
     def __init__(self, fmt, k, v, k_scale=None, v_scale=None):
-        import torch
-
         if fmt not in KV_FORMATS:
             raise ValueError(f"cache format {fmt!r}: one of {', '.join(KV_FORMATS)}")
         want = {"f16": torch.float16, "bf16": torch.bfloat16}.get(fmt, torch.uint8)
@@ -97,6 +95,7 @@ class KvCache:
                 raise ValueError("qtea entry points take contiguous tensors")
             if not t.is_cuda or t.device != k.device:
                 raise ValueError("qtea entry points take device tensors, a cache's of one device")
+        self.device_index = k.get_device()
         ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
         self.desc = QteaKvCache(ptr(k), ptr(v), ptr(k_scale), ptr(v_scale), self.n_pages, KV_FORMATS[fmt], self.n_heads,
                                 self.head_dim, self.page_size)
@@ -104,8 +103,6 @@ class KvCache:
 
 def new_kv_cache(fmt, n_pages, page_size, n_heads, head_dim, device="cuda") -> KvCache:
     """A cache of zeros."""
-    import torch
-
     if fmt not in KV_FORMATS:
         raise ValueError(f"cache format {fmt!r}: one of {', '.join(KV_FORMATS)}")
     shape = (n_pages, n_heads, page_size)
@@ -118,19 +115,16 @@ def new_kv_cache(fmt, n_pages, page_size, n_heads, head_dim, device="cuda") -> K
 
 
 def _batch(cache, rows, q_start, kv_len, page_table):
-    import torch
-
-    i32 = torch.int32
-    if q_start.dtype != i32 or kv_len.dtype != i32 or page_table.dtype != i32:
+    if q_start.dtype is not _I32 or kv_len.dtype is not _I32 or page_table.dtype is not _I32:
         raise ValueError("q_start, kv_len and page_table are int32")
-    n = kv_len.numel()
-    if q_start.numel() != n + 1 or page_table.dim() != 2 or page_table.shape[0] != n:
+    n, table = kv_len.numel(), page_table.shape
+    if q_start.numel() != n + 1 or len(table) != 2 or table[0] != n:
         raise ValueError("q_start has one entry more than kv_len, page_table one row per entry of it")
     if not (q_start.is_contiguous() and kv_len.is_contiguous() and page_table.is_contiguous()):
         raise ValueError("qtea entry points take contiguous tensors")
-    if not (q_start.device == kv_len.device == page_table.device == cache.k.device):
+    if not (q_start.get_device() == kv_len.get_device() == page_table.get_device() == cache.device_index):
         raise ValueError("qtea entry points take tensors of the cache's device")
-    return QteaKvBatch(q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), rows, n, page_table.shape[1])
+    return QteaKvBatch(q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), rows, n, table[1])
 
 
 def _rows(cache, t, heads, what):
@@ -140,20 +134,20 @@ def _rows(cache, t, heads, what):
         raise ValueError(f"{what}: [tokens][{heads}][{dim}], got {list(shape)}")
     if stride[2] != 1 or (stride[1] != dim and heads > 1):
         raise ValueError(f"{what}: a token's heads and channels are contiguous")
-    if t.device != cache.k.device:
+    if t.get_device() != cache.device_index:
         raise ValueError(f"{what}: a tensor of the cache's device")
     return max(stride[0], heads * dim) if shape[0] <= 1 else stride[0]
 
 
 def _dense(name, cache, k, v, q_start, kv_len, page_table, stream):
-    q = _package()
+    q = _q
     ks, vs = _rows(cache, k, cache.n_heads, "k"), _rows(cache, v, cache.n_heads, "v")
     if k.dtype != v.dtype or k.shape[0] != v.shape[0]:
         raise ValueError("k and v: one type, one number of tokens")
     b = _batch(cache, k.shape[0], q_start, kv_len, page_table)
     if k.shape[0] == 0:
         return
-    q._check(getattr(q.load(), name)(cache.desc, b, k.data_ptr(), v.data_ptr(), _type(k, "k and v"), ks, vs, _stream(stream)), name)
+    q._check(getattr(q.load(), name)(cache.desc, b, k.data_ptr(), v.data_ptr(), _type(k, "k and v"), ks, vs, _stream(stream, cache.device_index)), name)
 
 
 def qtea_kv_append(cache: KvCache, k, v, q_start, kv_len, page_table, stream=None):
@@ -170,15 +164,13 @@ def qtea_kv_read(cache: KvCache, q_start, kv_len, page_table, k, v, stream=None)
 
 
 def qtea_attention_workspace_bytes(n_q_heads: int, head_dim: int) -> int:
-    q, out = _package(), _i64(0)
+    q, out = _q, _i64(0)
     q._check(q.load().qtea_attention_workspace_bytes(int(n_q_heads), int(head_dim), ctypes.byref(out)), "qtea_attention_workspace_bytes")
     return out.value
 
 
 def new_attention_workspace(n_q_heads: int, head_dim: int, device="cuda"):
     """A zero-filled workspace for qtea_paged_attention."""
-    import torch
-
     return torch.zeros(qtea_attention_workspace_bytes(n_q_heads, head_dim), dtype=torch.uint8, device=device)
 
 
@@ -187,31 +179,29 @@ def qtea_paged_attention(cache: KvCache, Q, q_start, kv_len, page_table, out, wo
     [head_dim] (fp16 or bf16), over the cache that already holds them, into
     `out` (as Q).  scale: 1 / sqrt(head_dim) unless given; window: positions a
     row sees, 0 for all."""
-    q = _package()
+    q = _q
     if Q.dim() != 3 or Q.shape != out.shape or Q.dtype != out.dtype:
         raise ValueError("Q and out: one type, one shape [tokens][heads][channels]")
     heads = Q.shape[1]
     qs, os_ = _rows(cache, Q, heads, "Q"), _rows(cache, out, heads, "out")
     b = _batch(cache, Q.shape[0], q_start, kv_len, page_table)
-    if workspace.device != cache.k.device or not workspace.is_contiguous():
+    if workspace.get_device() != cache.device_index or not workspace.is_contiguous():
         raise ValueError("workspace: a contiguous tensor of the cache's device")
     if Q.shape[0] == 0:
         return
     q._check(q.load().qtea_paged_attention(cache.desc, b, Q.data_ptr(), out.data_ptr(), _type(Q, "Q and out"), heads, qs, os_,
                                            cache.head_dim ** -0.5 if scale is None else scale, window, workspace.data_ptr(),
-                                           workspace.numel() * workspace.element_size(), _stream(stream)), "qtea_paged_attention")
+                                           workspace.numel() * workspace.element_size(), _stream(stream, cache.device_index)), "qtea_paged_attention")
 
 
 def qtea_verify_workspace_bytes(n_seq: int) -> int:
-    q, out = _package(), _i64(0)
+    q, out = _q, _i64(0)
     q._check(q.load().qtea_verify_workspace_bytes(int(n_seq), ctypes.byref(out)), "qtea_verify_workspace_bytes")
     return out.value
 
 
 def new_verify_workspace(n_seq: int, device="cuda"):
     """A zero-filled workspace for qtea_verify_draft."""
-    import torch
-
     return torch.zeros(qtea_verify_workspace_bytes(n_seq), dtype=torch.uint8, device=device)
 
 
@@ -223,26 +213,26 @@ def qtea_verify_draft(target, draft, tokens, q_start, u_accept, u_sample, n_acce
     u_accept fp32 [drafts], q_start int32 [n_seq + 1] over the target's rows,
     u_sample fp32 [n_seq]; outputs n_accepted int32 [n_seq] and out_tokens
     int32 [n_seq][max_draft + 1]."""
-    import torch
-
-    q = _package()
+    q = _q
     n_seq, n_drafts = u_sample.numel(), tokens.numel()
     if target.dim() != 2 or (target.stride(1) != 1 and target.shape[1] > 1):
         raise ValueError("target: [rows][vocab], a row contiguous")
     vocab = target.shape[1]
-    if draft is not None and (draft.dim() != 2 or draft.shape != (n_drafts, vocab) or draft.dtype != target.dtype or (draft.stride(1) != 1 and vocab > 1 and n_drafts > 0)):
+    if draft is not None and (draft.dim() != 2 or tuple(draft.shape) != (n_drafts, vocab) or draft.dtype != target.dtype or (draft.stride(1) != 1 and vocab > 1 and n_drafts > 0)):
         raise ValueError("draft: a row of the target's type and vocabulary for each drafted token")
-    i32, f32 = torch.int32, torch.float32
-    if tokens.dtype != i32 or q_start.dtype != i32 or n_accepted.dtype != i32 or out_tokens.dtype != i32 or u_accept.dtype != f32 or u_sample.dtype != f32:
+    if (tokens.dtype is not _I32 or q_start.dtype is not _I32 or n_accepted.dtype is not _I32 or out_tokens.dtype is not _I32
+            or u_accept.dtype is not _F32 or u_sample.dtype is not _F32):
         raise ValueError("tokens, q_start, n_accepted and out_tokens are int32, u_accept and u_sample fp32")
     if q_start.numel() != n_seq + 1 or n_accepted.numel() != n_seq or u_accept.numel() != n_drafts or out_tokens.dim() != 2 or out_tokens.shape[0] != n_seq or out_tokens.shape[1] < 1:
         raise ValueError("one u_sample, n_accepted and row of out_tokens per sequence, one u_accept per draft, one q_start more than sequences")
-    for t in (target, draft, tokens, q_start, u_accept, u_sample, n_accepted, out_tokens, workspace):
-        if t is not None and (t.device != target.device or not t.is_cuda):
-            raise ValueError("qtea entry points take device tensors, one call's of one device")
+    dev = target.get_device()
+    if dev < 0 or (draft is not None and draft.get_device() != dev):
+        raise ValueError("qtea entry points take device tensors, one call's of one device")
     for t in (tokens, q_start, u_accept, u_sample, n_accepted, out_tokens, workspace):
         if not t.is_contiguous():
             raise ValueError("qtea entry points take contiguous tensors")
+        if t.get_device() != dev:
+            raise ValueError("qtea entry points take device tensors, one call's of one device")
     if n_seq == 0:
         return
     one = lambda t: max(t.stride(0), vocab) if t.shape[0] <= 1 else t.stride(0)  # noqa: E731
@@ -250,5 +240,5 @@ def qtea_verify_draft(target, draft, tokens, q_start, u_accept, u_sample, n_acce
                                         one(target), 0 if draft is None else one(draft), tokens.data_ptr(), q_start.data_ptr(),
                                         u_accept.data_ptr(), u_sample.data_ptr(), n_seq, target.shape[0], n_drafts,
                                         out_tokens.shape[1] - 1, n_accepted.data_ptr(), out_tokens.data_ptr(),
-                                        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)),
+                                        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream, dev)),
              "qtea_verify_draft")
