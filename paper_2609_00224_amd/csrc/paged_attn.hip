@@ -769,7 +769,7 @@ __device__ __forceinline__ u32x2 lds_read_transposed(const char* p) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
 }
 
-template <int DP, int FMT, class T>
+template <int DP, int FMT, class T, bool EX>  // (EX as above)
 __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attn_tile_kernel(const AttnArgs a, int parts) {
   using ST = Stage<DP, FMT>;
   constexpr int KT = ST::kTok, NB = ST::kBlocks, CB = DP / 32, NL = ST::kLoads;
@@ -778,7 +778,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attn_tile_kernel(
   __shared__ int s_odd, s_last;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n32 = lane & 31, half = lane >> 5;
-  const int D = a.dim, H = a.heads, G = a.group;
+  const int D = EX ? DP : a.dim, H = a.heads, G = a.group;
   const int rowb = FMT == 0 ? 2 * D : (FMT == 1 ? D : D / 2), nb = D / 32;
   const int capacity = a.b.max_pages << a.page_shift, pmask = (1 << a.page_shift) - 1;
 
@@ -840,7 +840,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attn_tile_kernel(
   // staging: this thread's chunks of a tile
   const int32_t* table = a.b.page_table + int64_t(s) * a.b.max_pages;
   u32x4 rk[NL], rv[NL];
-  uint32_t sk[NL], sv[NL];
+  uint32_t sk[NL] = {}, sv[NL] = {};
   int pg[NL];
   auto chunk_of = [&](int p, int& tok, int& cc) {
     const int idx = tid + kThreads * p;
@@ -873,30 +873,30 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attn_tile_kernel(
       else if constexpr (FMT == 0) sk[p] = 0;
     }
   };
-  auto store = [&](int t, int buf) {
-    const bool edge = t * KT + KT > hi_min || t * KT < lo_max;
+  // (PLAIN: every token of the tile is one that all rows see, and has a page)
+  auto store_as = [&](int t, int buf, auto plain) {
+    constexpr bool PLAIN = decltype(plain)::value;
     bool odd = false;
 #pragma unroll
     for (int p = 0; p < NL; ++p) {
       int tok, cc;
       if (!chunk_of(p, tok, cc)) continue;
-      const int at = t * KT + tok;
-      const bool none = cc * ST::kChunk >= D;  // channels that pad the tile
-      const bool gone = (sk[p] >> 16) != 0;
+      const bool none = !EX && cc * ST::kChunk >= D;  // channels that pad the tile
+      const bool past = !PLAIN && t * KT + tok >= hi_max, gone = !PLAIN && (sk[p] >> 16) != 0;
 #pragma unroll
       for (int i = 0; i < ST::kChunk / 8; ++i) {
         const uint32_t wk[4] = {rk[p][0], rk[p][1], rk[p][2], rk[p][3]}, wv[4] = {rv[p][0], rv[p][1], rv[p][2], rv[p][3]};
         uint32_t k4[4], v4[4];
-        decode_words<FMT, T>(wk, i, FMT ? scale_of(sk[p] & 255u) : 1.0f, k4);
+        decode_words<FMT, T>(wk, i, FMT ? scale_of(PLAIN ? sk[p] : sk[p] & 255u) : 1.0f, k4);
         decode_words<FMT, T>(wv, i, FMT ? scale_of(sv[p]) : 1.0f, v4);
-        if (none || (edge && at >= hi_max)) {
+        if (none || past) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) k4[e] = v4[e] = 0;
         } else if (gone) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) k4[e] = 0x7fff7fffu, v4[e] = 0;
         }
-        if (edge) {
+        if (!PLAIN) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const uint32_t fm = finite_mask<T>(v4[e]);
@@ -911,6 +911,13 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attn_tile_kernel(
     }
     if (odd) s_odd = 1;
   };
+  auto store = [&](int t, int buf) {
+    bool gone = false;
+#pragma unroll
+    for (int p = 0; p < NL; ++p) gone |= (sk[p] >> 16) != 0;
+    if (t * KT + KT > hi_min || t * KT < lo_max || __ballot(gone) != 0) store_as(t, buf, std::false_type());
+    else store_as(t, buf, std::true_type());
+  };
 
   if (tid == 0) s_odd = 0;
   __syncthreads();
@@ -922,6 +929,15 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attn_tile_kernel(
     if (ta + 1 < tb) load(ta + 1);
     if (ta + 2 < tb) pages(ta + 2);
   }
+  // (the queries are here before the loop: in it, a wait for them would be one for every load)
+#pragma unroll
+  for (int j = 0; j < DP / 16; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      uint32_t x = qf[j][e];
+      asm volatile("" : "+v"(x));
+      qf[j][e] = x;
+    }
   __syncthreads();
 
   const uint32_t k_at = k_place<DP>(n32, half);
@@ -1152,7 +1168,9 @@ int qtea_paged_attention(const qtea_kv_cache* cache, const qtea_kv_batch* batch,
     constexpr int DP = decltype(dp)::value, FMT = decltype(fmt)::value;
     using T = decltype(ty);
     if (many) {
-      hipLaunchKernelGGL((attn_tile_kernel<DP, FMT, T>), dim3(uint32_t(tasks * H * parts)), block, 0, st, a, parts);
+      const dim3 wgs(uint32_t(tasks * H * parts));
+      if (D == DP) hipLaunchKernelGGL((attn_tile_kernel<DP, FMT, T, true>), wgs, block, 0, st, a, parts);
+      else hipLaunchKernelGGL((attn_tile_kernel<DP, FMT, T, false>), wgs, block, 0, st, a, parts);
       return;
     }
     auto rows_launch = [&](auto r) {
