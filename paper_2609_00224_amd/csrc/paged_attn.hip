@@ -1,4 +1,25 @@
 // Causal attention of a batch's newest tokens over the paged cache.
+//
+// One pass over the cached tokens with a running maximum m and sum l per row
+// (a row is a new token and a query head): a tile of tokens gives scores
+// s = q . k and weights w = 2^(s c - m), c = scale log2(e), and adds w v to the
+// row's sums; m moves only when a score passes it by 8 (the sums are then
+// scaled), and the sums are divided by l at the end.  Both products run on the
+// matrix cores with the tokens (K, V^T) as the left operand and the rows as
+// the right one, so that a score, its weight and the operand of the second
+// product are the same register of the same lane: nothing is exchanged
+// between lanes on the way.  Quantized values are decoded to `type` by the
+// hardware's scaled conversions, which is exact.  Sums, maxima and scores are
+// fp32; the weights are rounded to `type` for the second product, as every
+// factor of a 16-bit matrix product is (their sum l is not: the result is off
+// by one more rounding to `type` at most).
+//
+// Two kernels, by the rows that a sequence has on average.  Up to 64 (32 past
+// 128 channels) the cached bytes bound the call and attn_rows_kernel keeps
+// them in registers from the load to the product; beyond, the products do,
+// and attn_tile_kernel shares tiles in LDS among 128 rows.  On both sides of the
+// line (16 sequences, nine tokens of five query heads a group on average, up
+// to 9000 bf16 positions): 89 us against 195.
 #include <math.h>
 
 #include <algorithm>
@@ -36,7 +57,24 @@ struct AttnArgs {
 // (new tokens x the query heads that share the head).  A task's tokens are
 // split into chunks, one to a workgroup, so that every CU has its workgroups
 // busy for about as long; a chunk's tokens are dealt to the waves, 32 at a
-// time, and each wave keeps its own sums until the end.
+// time, and each wave keeps its own sums until the end.  (Equal runs of units
+// whatever task they are of balance better but have workgroups change tasks:
+// 76 us against 73 for 16 ragged sequences, 49 against 34 for four with drafts.)
+//
+// A lane's loads: of K, channels of one token, 64 contiguous bytes of it per
+// four lanes (the order of the channels is free, as the queries have it too);
+// of V, DP / 16 neighbouring channels of 8 tokens, a token's row being the 16
+// lanes of a group.  V's pairs of channels per token become pairs of tokens
+// per channel by one byte permutation a word.
+//
+// Bound by HBM for long histories (one token over 260001 positions in E2M1,
+// 283 MB: 61 us; 16 tokens over up to 16000 in E4M3, 360 MB: 73 us; each
+// further position at 6.0 to 6.3 TB/s), below that by the chain of dependent
+// reads: lengths, pages, values, parts (one token over 700: 10.4 us, of which
+// 1.1 are the launch, 1.5 the chunk search, 1.1 the pages, 2 the one tile, 0.9
+// the waves' join, 3 the arrival and the parts).  A wave of 32 rows reads
+// each value once, which is faster than two waves of 16 that read it from the
+// L1 and L2 (34 us against 53 for four sequences' drafts).
 // ---------------------------------------------------------------------------
 
 // The work of sequence s: `nqt` row tasks per head, each of `cnt` units of
@@ -732,8 +770,19 @@ __global__ __launch_bounds__(kRowThreads, rows_per_cu(DP, FMT, R)) void attn_row
 
 // ---------------------------------------------------------------------------
 // Many rows: a task is one sequence, one key/value head and 128 rows, 32 per
-// wave; the workgroup stages tiles of tokens through LDS for its four waves.
-// Where there are few tasks their tokens are split into `parts`.
+// wave; the workgroup stages tiles of 64 tokens (32 past 128 channels) through
+// LDS, decoded, for its four waves: two tiles, one being read while the next
+// comes in by way of registers.  Where there are few tasks their tokens are
+// split into `parts`.
+//
+// Bound by instruction issue: for 64 tokens x 32 rows x 128 channels a wave
+// issues 32 products (1024 cycles of its SIMD) and about 265 vector
+// instructions (1440 cycles, of them 512 for the exponentials), and the two
+// waves of a SIMD overlap little of the one with the other: 37 % of the
+// cycles have a product in the matrix core, 47 % a vector instruction.  A
+// 2048-token chunk over 12345 positions, 32 heads, E4M3: 440 us, 864 TFLOP/s
+// (fp16 cache 816, E2M1 902); six prompts of up to 4000 tokens, 64 channels,
+// window 1024, bf16: 108 us, 594 TFLOP/s of the pairs in the windows.
 // ---------------------------------------------------------------------------
 constexpr int kTaskRows = 128;
 constexpr int kMinPart = 4;   // tiles of a part, at least
@@ -1068,12 +1117,68 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attn_tile_kernel(
     }
   }
   if (!last_to_arrive(a.counters + id * kCounterWords, used, &s_last)) return;
-  join_parts<DP, kTaskRows, kThreads>(a, a.part_ml, slot0, 1, used, nrow, reinterpret_cast<float*>(&s_k[0][0]), [&](int row, int ch, const Joined& j) {
-    const int r = r0 + row, i = r / G;
-    const float inv = pos0 + i < 0 && j.L == 0.0f ? 0.0f : 1.0f / j.L;
-    uint16_t* to = a.out + (int64_t(q.first) + i) * a.out_stride + int64_t(h * G + (r - i * G)) * D + ch;
-    *reinterpret_cast<u32x2*>(to) = u32x2{T::pack(j.acc[0] * inv, j.acc[1] * inv), T::pack(j.acc[2] * inv, j.acc[3] * inv)};
-  });
+  // With up to 128 rows a thread has many items, so the parts' factors are
+  // found once, in LDS, and two items' sums are asked for together (a
+  // 200-token chunk in nine parts: 98 us, 110 with join_parts).
+  float* s_f = reinterpret_cast<float*>(&s_k[0][0]);  // [rows][parts]: maxima, then factors
+  float* s_w = s_f + kTaskRows * kMaxParts;           // sums
+  static_assert(2 * kTaskRows * kMaxParts * 4 <= sizeof(s_k), "the parts' maxima and sums in LDS");
+#pragma unroll 4
+  for (int e = tid; e < kTaskRows * used; e += kThreads) {
+    const int p = e / kTaskRows, row = min(e % kTaskRows, nrow - 1);
+    const float* from = a.part_ml + (slot0 + p) * (2 * kTaskRows) + row;
+    s_f[e % kTaskRows * kMaxParts + p] = qtea_detail::load_coherent(from);
+    s_w[e % kTaskRows * kMaxParts + p] = qtea_detail::load_coherent(from + kTaskRows);
+  }
+  __syncthreads();
+  if (tid < kTaskRows) {
+    float* f = s_f + tid * kMaxParts;
+    float* w = s_w + tid * kMaxParts;
+    float M = -INFINITY, L = 0.0f;
+    for (int p = 0; p < used; ++p) M = fmaxf(M, f[p]);
+    for (int p = 0; p < used; ++p) {
+      f[p] = f[p] == M ? 1.0f : __builtin_amdgcn_exp2f(f[p] - M);
+      L += w[p] * f[p];
+    }
+    w[0] = L;
+  }
+  __syncthreads();
+  const int quads = D / 4, items = nrow * quads;
+  constexpr int kItems = 2, kBatch = 8;
+  for (int e0 = tid; e0 < items; e0 += kItems * kThreads) {
+    f32x4 acc[kItems];
+    int row[kItems], ch[kItems];
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+      const int e = min(e0 + k * kThreads, items - 1);
+      row[k] = e / quads, ch[k] = (e - row[k] * quads) * 4;
+      acc[k] = f32x4{0, 0, 0, 0};
+    }
+    for (int p0 = 0; p0 < used; p0 += kBatch) {
+      f32x2 x[kItems][kBatch], y[kItems][kBatch];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i)
+#pragma unroll
+        for (int k = 0; k < kItems; ++k) {
+          const float* po = a.part + (slot0 + min(p0 + i, used - 1)) * (kTaskRows * DP) + row[k] * DP + ch[k];
+          x[k][i] = load_coherent2(po), y[k][i] = load_coherent2(po + 2);
+        }
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i)
+        if (p0 + i < used) {
+#pragma unroll
+          for (int k = 0; k < kItems; ++k) acc[k] += f32x4{x[k][i][0], x[k][i][1], y[k][i][0], y[k][i][1]} * s_f[row[k] * kMaxParts + p0 + i];
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+      if (e0 + k * kThreads >= items) continue;
+      const int r = r0 + row[k], i = r / G;
+      const float L = s_w[row[k] * kMaxParts], inv = pos0 + i < 0 && L == 0.0f ? 0.0f : 1.0f / L;
+      uint16_t* to = a.out + (int64_t(q.first) + i) * a.out_stride + int64_t(h * G + (r - i * G)) * D + ch[k];
+      *reinterpret_cast<u32x2*>(to) = u32x2{T::pack(acc[k][0] * inv, acc[k][1] * inv), T::pack(acc[k][2] * inv, acc[k][3] * inv)};
+    }
+  }
 }
 
 int device_cus() {
