@@ -128,7 +128,7 @@ int qtea_kv_read(const qtea_kv_cache* cache, const qtea_kv_batch* batch, void* k
  * It holds arrival counters and partial rows, and must be zero-filled once
  * before its first use (qtea_workspace_init); every call that runs to
  * completion leaves the counters at zero.  Calls that may overlap in time
- * must not share one.
+ * must not share one, and no other entry point may use it.
  */
 int qtea_attention_workspace_bytes(int n_q_heads, int head_dim, int64_t* out_bytes);
 
@@ -163,8 +163,12 @@ int qtea_paged_attention(const qtea_kv_cache* cache, const qtea_kv_batch* batch,
                          int n_q_heads, int64_t q_stride, int64_t out_stride, float scale, int window, void* workspace,
                          int64_t workspace_bytes, void* stream);
 
-/* Workspace bytes of qtea_verify_draft for n_seq sequences (zero-filled once
- * and shared as the attention's). */
+/*
+ * Workspace bytes of qtea_verify_draft for n_seq sequences.  As the
+ * attention's it holds arrival counters, is zero-filled once, and must not be
+ * shared by calls that may overlap in time, nor with another entry point.  One
+ * made for n_seq sequences serves every smaller call too, in any order.
+ */
 int qtea_verify_workspace_bytes(int n_seq, int64_t* out_bytes);
 
 /*

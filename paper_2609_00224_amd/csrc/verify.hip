@@ -22,7 +22,10 @@ constexpr int kThreads = 256;
 constexpr int kMaxSlices = 64;      // a wave scans their sums
 constexpr int kBlock = 8 * kThreads;  // vocabulary entries of one step; slices are whole blocks
 constexpr int kTargetBlocks = 2048; // workgroups that keep HBM busy
-constexpr int64_t kCounterBytes = 128;  // a line each: arrivals at one line are served one after another
+// A sequence's record in the workspace: its arrival counter and its slices'
+// sums, at one place whatever the call's number of sequences.  (The counter has
+// a line of its own: arrivals at one line are served one after another.)
+constexpr int64_t kCounterBytes = 128;
 constexpr int64_t kSeqBytes = kCounterBytes + kMaxSlices * 16;
 
 struct VerifyArgs {
@@ -35,8 +38,7 @@ struct VerifyArgs {
   const float* u_sample;
   int32_t* n_accepted;
   int32_t* out_tokens;
-  char* counters;  // [n_seq], kCounterBytes apart
-  uint64_t* sums;  // [n_seq][kMaxSlices][2]: of max(P - Q, 0), of P
+  char* records;  // [n_seq], kSeqBytes apart: the counter, then [kMaxSlices][2] sums of max(P - Q, 0) and of P
   int32_t vocab, n_seq, n_rows, n_drafts, max_draft, slices, slice;
 };
 
@@ -177,7 +179,8 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(const VerifyArgs a) {
   sw = readlane64(wave_scan64(sw), 63), sp = readlane64(wave_scan64(sp), 63);
   if (lane == 0) s_sum[wave][0] = sw, s_sum[wave][1] = sp;
   __syncthreads();
-  uint64_t* sums = a.sums + int64_t(s) * (2 * kMaxSlices);
+  char* record = a.records + int64_t(s) * kSeqBytes;
+  uint64_t* sums = reinterpret_cast<uint64_t*>(record + kCounterBytes);
   if (tid == 0) {
     const uint64_t tw = s_sum[0][0] + s_sum[1][0] + s_sum[2][0] + s_sum[3][0], tp = s_sum[0][1] + s_sum[1][1] + s_sum[2][1] + s_sum[3][1];
     __hip_atomic_store(sums + 2 * slice, tw, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -185,7 +188,7 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(const VerifyArgs a) {
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0);  // the sums are there before their arrival is counted
     asm volatile("" ::: "memory");
-    uint32_t* counter = reinterpret_cast<uint32_t*>(a.counters + s * kCounterBytes);
+    uint32_t* counter = reinterpret_cast<uint32_t*>(record);
     const uint32_t before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     const bool last = before == uint32_t(a.slices - 1);
     if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -274,8 +277,7 @@ int qtea_verify_draft(const void* target, const void* draft, int type, int64_t v
   a.target_stride = target_stride * size, a.draft_stride = draft_stride * size;
   a.tokens = tokens, a.q_start = q_start, a.u_accept = u_accept, a.u_sample = u_sample;
   a.n_accepted = n_accepted, a.out_tokens = out_tokens;
-  a.counters = static_cast<char*>(workspace);
-  a.sums = reinterpret_cast<uint64_t*>(a.counters + int64_t(n_seq) * kCounterBytes);
+  a.records = static_cast<char*>(workspace);
   a.vocab = int32_t(vocab), a.n_seq = n_seq, a.n_rows = int32_t(n_rows), a.n_drafts = int32_t(n_drafts), a.max_draft = max_draft;
   // Slices of whole blocks: as many as fill the chip, at most kMaxSlices.
   const int64_t want = std::min<int64_t>(std::max<int64_t>(1, kTargetBlocks / n_seq), kMaxSlices);
