@@ -118,7 +118,8 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(const VerifyArgs a) {
     if (t < s) some = min(max(a.q_start[t + 1], 0), a.n_rows) > min(max(a.q_start[t], 0), a.n_rows);
     with += __popcll(__ballot(some));
   }
-  const int d0 = first - with, n = min(rows - 1, a.max_draft);
+  const int base = min(max(a.q_start[0], 0), a.n_rows);  // (rows before the first sequence have no drafts)
+  const int d0 = first - base - with, n = min(rows - 1, a.max_draft);
   // the first rejected draft, 64 at a time (every wave finds it)
   int acc = n;
   for (int i0 = 0; i0 < n; i0 += 64) {

@@ -22,3 +22,19 @@ def test_one_verification_workspace_serves_batches_of_any_size():
         got, want = _run(x, 3, ws=ws), _want(x, 3)
         np.testing.assert_array_equal(got[0], want[0])
         np.testing.assert_array_equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("deterministic", [False, True])
+@pytest.mark.parametrize("ahead", [1, 4])
+def test_the_first_sequences_drafts_come_first_wherever_its_rows_start(ahead, deterministic):
+    """Target rows of no sequence before the first: the drafts do not move."""
+    rng = np.random.default_rng([21, ahead])
+    x = _inputs(rng, [2, 0, 3, 1], 500, "f32")
+    if deterministic:
+        del x["draft"]
+    want = _want(x, 3)
+    x["target"] = torch.cat((torch.rand((ahead, 500)), x["target"]))
+    x["q_start"] = x["q_start"] + ahead
+    got = _run(x, 3)
+    np.testing.assert_array_equal(got[0], want[0])
+    np.testing.assert_array_equal(got[1], want[1])
