@@ -192,6 +192,7 @@ int qtea_verify_workspace_bytes(int n_seq, int64_t* out_bytes);
  *   mass at all.
  *
  *   target      device [rows][vocab] of `type`, target_stride elements apart
+ *               (not read, and possibly NULL, where n_rows is 0)
  *   draft       the same for the drafts, draft_stride apart; NULL: every
  *               drafted token had probability 1 (a deterministic draft)
  *   tokens      device int32 [drafts]; one outside [0, vocab) is rejected

@@ -261,10 +261,10 @@ int qtea_verify_draft(const void* target, const void* draft, int type, int64_t v
                       int64_t draft_stride, const int32_t* tokens, const int32_t* q_start, const float* u_accept,
                       const float* u_sample, int n_seq, int64_t n_rows, int64_t n_drafts, int max_draft,
                       int32_t* n_accepted, int32_t* out_tokens, void* workspace, int64_t workspace_bytes, void* stream) {
-  if (!target || !q_start || !u_sample || !n_accepted || !out_tokens || !workspace) return QTEA_ERR_INVALID_ARG;
+  if (!q_start || !u_sample || !n_accepted || !out_tokens || !workspace) return QTEA_ERR_INVALID_ARG;
   if (type < QTEA_F16 || type > QTEA_F32 || vocab < 1 || vocab > (1 << 24) || n_seq < 1 || max_draft < 0 || max_draft > 1023) return QTEA_ERR_INVALID_ARG;
   if (n_rows < 0 || n_rows > INT32_MAX || n_drafts < 0 || n_drafts > INT32_MAX) return QTEA_ERR_INVALID_ARG;
-  if (n_drafts > 0 && (!tokens || !u_accept)) return QTEA_ERR_INVALID_ARG;
+  if ((n_rows > 0 && !target) || (n_drafts > 0 && (!tokens || !u_accept))) return QTEA_ERR_INVALID_ARG;
   if (target_stride < vocab || target_stride > (INT64_MAX >> 34)) return QTEA_ERR_INVALID_ARG;
   if (draft && (draft_stride < vocab || draft_stride > (INT64_MAX >> 34))) return QTEA_ERR_INVALID_ARG;
   const int64_t size = type == QTEA_F32 ? 4 : 2;

@@ -38,3 +38,12 @@ def test_the_first_sequences_drafts_come_first_wherever_its_rows_start(ahead, de
     got = _run(x, 3)
     np.testing.assert_array_equal(got[0], want[0])
     np.testing.assert_array_equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("with_draft", [False, True])
+def test_a_verification_without_any_rows(with_draft):
+    z = lambda *s, dt=torch.int32: torch.zeros(s, dtype=dt, device="cuda")  # noqa: E731
+    acc, out = torch.full((3,), 99, dtype=torch.int32, device="cuda"), torch.full((3, 3), 99, dtype=torch.int32, device="cuda")
+    rows = z(0, 50, dt=torch.float32)
+    q.qtea_verify_draft(rows, rows if with_draft else None, z(0), z(4), z(0, dt=torch.float32), z(3, dt=torch.float32), acc, out, q.new_verify_workspace(3))
+    assert (acc == 0).all() and (out == -1).all()
