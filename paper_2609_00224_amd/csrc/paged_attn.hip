@@ -239,7 +239,7 @@ __device__ __forceinline__ float not_finite_value(const AttnArgs& a, int64_t row
   uint32_t w;
   if constexpr (FMT == 0) w = reinterpret_cast<const uint16_t*>(a.v)[row * a.dim + c];
   else if constexpr (FMT == 1) w = T::template e4m3<false>(a.v[row * a.dim + c], scale_of(a.vs[row * (a.dim / 32) + c / 32]));
-  else w = T::template e2m1<0>(a.v[row * (a.dim / 2) + c / 2], scale_of(a.vs[row * (a.dim / 32) + c / 32]));  // (all of a block or none)
+  else w = T::template e2m1<0>(uint32_t(a.v[row * (a.dim / 2) + c / 2]) >> (4 * (c & 1)), scale_of(a.vs[row * (a.dim / 32) + c / 32]));
   const float v = float(__builtin_bit_cast(typename T::pair, w)[0]);
   return fabsf(v) < INFINITY ? 0.0f : v;
 }

@@ -47,3 +47,58 @@ def test_a_verification_without_any_rows(with_draft):
     rows = z(0, 50, dt=torch.float32)
     q.qtea_verify_draft(rows, rows if with_draft else None, z(0), z(4), z(0, dt=torch.float32), z(3, dt=torch.float32), acc, out, q.new_verify_workspace(3))
     assert (acc == 0).all() and (out == -1).all()
+
+
+def _large_scale_case(new, window, fmt, qtype, byte, seed):
+    """One sequence of 150 positions, the last `new` of them new."""
+    rng = np.random.default_rng([22, new, window, byte, seed])
+    p = Paged(rng, [(150, new)], 2, 64, 64, fmt)
+    p.qtype = qtype
+    Q = rounded(rng.standard_normal((new, 4, 64)), qtype)
+    return rng, p, Q
+
+
+def _attend(p, Q, window, cache):
+    out = torch.full(Q.shape, 7.0, dtype=TORCH[p.qtype], device="cuda")
+    q.qtea_paged_attention(cache, torch.from_numpy(Q).to(TORCH[p.qtype]).cuda(), *p.meta(), out, q.new_attention_workspace(Q.shape[1], p.dim), window=window)
+    return out.double().cpu().numpy()
+
+
+def _poison(cache, fmt, page, off, byte, codes):
+    """Token's V: scale bytes and codes ([32] per block, the same for all)."""
+    cache.v_scale[page, :, off] = byte
+    row = np.concatenate([codes] * 2)
+    if fmt == "e2m1":
+        row = row[0::2] | (row[1::2] << 4)
+    cache.v[page, :, off] = torch.from_numpy(row.astype(np.uint8)).cuda()
+
+
+# Codes of a block: the largest, small and zero ones side by side.
+CODES = {"e4m3": np.array([0x7e, 0x00, 0x08, 0xfe] * 8, np.uint8), "e2m1": np.array([7, 0, 1, 15, 1, 7, 0, 9] * 4, np.uint8)}
+
+
+def _check_seen(new, qtype, fmt, byte):
+    """The newest token's V, which only the last row sees: a channel whose
+    value rounds to an infinity of the type is that infinity, the others are
+    finite, and no other row changes."""
+    rng, p, Q = _large_scale_case(new, 0, fmt, qtype, byte, 1)
+    cache = p.cache()
+    want = _attend(p, Q, 0, cache)
+    pg, off = p.places(0, 0, 150)
+    _poison(cache, fmt, int(pg[149]), int(off[149]), byte, CODES[fmt])
+    got = _attend(p, Q, 0, cache)
+    np.testing.assert_array_equal(got[:-1], want[:-1])
+    value = sv.decode(np.concatenate([CODES[fmt]] * 2), np.array([byte] * 2, np.uint8), fmt)
+    as_type = torch.from_numpy(value).to(TORCH[qtype]).double().numpy()
+    inf = np.isinf(as_type)
+    np.testing.assert_array_equal(got[-1][:, inf], np.broadcast_to(as_type[inf], (4, int(inf.sum()))))
+    assert not np.isnan(got[-1]).any()
+    # a share of a finite value and of the others' values
+    assert (np.abs(got[-1][:, ~inf]) <= 1.01 * (np.abs(as_type[~inf]) + np.abs(p.v[0]).max())).all()
+
+
+@pytest.mark.parametrize("byte", [135, 141, 200, 247, 253])
+@pytest.mark.parametrize("fmt", ["e4m3", "e2m1"])
+@pytest.mark.parametrize("qtype", ["f16", "bf16"])
+def test_seen_values_past_the_types_range_reach_their_rows_and_channels_many_rows(qtype, fmt, byte):
+    _check_seen(100, qtype, fmt, byte)
