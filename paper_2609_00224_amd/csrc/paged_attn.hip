@@ -193,13 +193,21 @@ __device__ __forceinline__ uint32_t finite_mask(uint32_t x) {
   return lo | hi;
 }
 
+// The largest scale byte under which no code passes the type's range.
+template <int FMT, class T>
+constexpr uint32_t kFiniteScale = (T::kExp == 0x7c00u ? 15 : 127) - (FMT == 1 ? 8 : 2) + 127;
+
 // Zeroes the values of N words of V codes that are not finite; whether there
-// were any.  (E4M3: NaN codes, and blocks of a NaN scale, E2M1's only kind.)
+// were any.  (E4M3: NaN codes; blocks of a NaN scale; codes that a large scale
+// takes past the type's range, which are looked for where there is such a scale.)
 template <int FMT, class T, int N>
 __device__ __forceinline__ bool drop_not_finite(uint32_t* w, uint32_t& scales, int shift) {
   uint32_t keep_all = 0xffffffffu, lost = 0;
+  bool large = false;
   if constexpr (FMT != 0) {
-    keep_all = __builtin_amdgcn_ubfe(scales, shift, 8) == 255u ? 0u : 0xffffffffu;
+    const uint32_t scale = __builtin_amdgcn_ubfe(scales, shift, 8);
+    keep_all = scale == 255u ? 0u : 0xffffffffu;
+    large = scale > kFiniteScale<FMT, T> && scale != 255u;
     scales &= keep_all;
     lost = ~keep_all;
   }
@@ -213,6 +221,18 @@ __device__ __forceinline__ bool drop_not_finite(uint32_t* w, uint32_t& scales, i
     }
     lost |= ~keep;
     w[i] &= keep;
+  }
+  if constexpr (FMT != 0) {
+    if (__builtin_expect(__ballot(large) != 0, 0)) {
+      constexpr int kPairs = FMT == 1 ? 2 : 4, kBits = FMT == 1 ? 8 : 4;  // of a word's codes
+#pragma unroll
+      for (int i = 0; i < kPairs * N; ++i) {
+        const uint32_t fm = finite_mask<T>(decode_pair<FMT, T>(w, i, scale_at(scales, shift)));
+        const uint32_t codes = ((fm & 0xffffu ? 0u : 1u) | (fm >> 16 ? 0u : 1u << kBits)) * ((1u << kBits) - 1);  // those to drop
+        lost |= codes;
+        w[i / kPairs] &= ~(codes << (2 * kBits * (i % kPairs)));
+      }
+    }
   }
   return lost != 0;
 }

@@ -102,3 +102,28 @@ def _check_seen(new, qtype, fmt, byte):
 @pytest.mark.parametrize("qtype", ["f16", "bf16"])
 def test_seen_values_past_the_types_range_reach_their_rows_and_channels_many_rows(qtype, fmt, byte):
     _check_seen(100, qtype, fmt, byte)
+
+
+@pytest.mark.parametrize("byte", [134, 135, 140, 141, 200, 246, 247, 252, 253, 254])
+@pytest.mark.parametrize("fmt", ["e4m3", "e2m1"])
+@pytest.mark.parametrize("qtype", ["f16", "bf16"])
+@pytest.mark.parametrize("new,window", [(1, 0), (6, 40), (100, 40)])
+def test_unseen_values_past_the_types_range_do_not_reach_a_row(new, window, qtype, fmt, byte):
+    """Past a sequence's end and below its window: any code and any scale."""
+    rng, p, Q = _large_scale_case(new, window, fmt, qtype, byte, 0)
+    cache = p.cache()
+    want = _attend(p, Q, window, cache)
+    pg, off = p.places(0, 0, 150)
+    unseen = [(int(p.table[0, 2]), o) for o in range(150 % 64, 64)]
+    unseen += [(int(pg[t]), int(off[t])) for t in range(max(0, 150 - new + 1 - window))] if window else []
+    for page, o in unseen:
+        _poison(cache, fmt, page, o, byte, rng.permutation(CODES[fmt]))
+    np.testing.assert_array_equal(_attend(p, Q, window, cache), want)
+
+
+@pytest.mark.parametrize("byte", [135, 141, 200, 247, 253])
+@pytest.mark.parametrize("fmt", ["e4m3", "e2m1"])
+@pytest.mark.parametrize("qtype", ["f16", "bf16"])
+@pytest.mark.parametrize("new", [2, 20])
+def test_seen_values_past_the_types_range_reach_their_rows_and_channels_few_rows(new, qtype, fmt, byte):
+    _check_seen(new, qtype, fmt, byte)
