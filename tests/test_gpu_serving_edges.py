@@ -7,7 +7,7 @@ import torch
 
 import oracle.serving as sv
 import paper_2609_00224_amd as q
-from tests.serving_cases import TORCH, Paged, attention_reference, rounded
+from tests.serving_cases import TORCH, Paged, attention_reference, pack, rounded
 from tests.test_gpu_verify_draft import _inputs, _run, _want
 
 pytestmark = pytest.mark.gpu
@@ -127,3 +127,31 @@ def test_unseen_values_past_the_types_range_do_not_reach_a_row(new, window, qtyp
 @pytest.mark.parametrize("new", [2, 20])
 def test_seen_values_past_the_types_range_reach_their_rows_and_channels_few_rows(new, qtype, fmt, byte):
     _check_seen(new, qtype, fmt, byte)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e2m1"])
+@pytest.mark.parametrize("qtype", ["f16", "bf16"])
+@pytest.mark.parametrize("new", [2, 100])
+def test_every_scale_and_code_of_a_token_that_one_row_sees(new, qtype, fmt):
+    """As above, all of a format's codes over 8 blocks, scales from where the
+    largest of them is finite to where every one but zero is not."""
+    rng = np.random.default_rng([26, new])
+    p = Paged(rng, [(90, new)], 1, 256, 32, fmt)
+    p.qtype = qtype
+    Q = rounded(rng.standard_normal((new, 1, 256)), qtype)
+    cache = p.cache()
+    want = _attend(p, Q, 0, cache)
+    pg, off = p.places(0, 0, 90)
+    codes = np.arange(256) if fmt == "e4m3" else np.tile(np.arange(16), 16)
+    codes = rng.permutation(codes).astype(np.uint8)
+    at = int(pg[89]), 0, int(off[89])
+    cache.v[at] = torch.from_numpy(pack(codes, fmt)).cuda()
+    for byte in range(132, 166) if qtype == "f16" else range(244, 256):
+        cache.v_scale[at] = byte
+        got = _attend(p, Q, 0, cache)
+        np.testing.assert_array_equal(got[:-1], want[:-1])
+        value = sv.decode(codes, np.full(8, byte, np.uint8), fmt)
+        as_type = torch.from_numpy(value).to(TORCH[qtype]).double().numpy()
+        wild = ~np.isfinite(as_type)
+        np.testing.assert_array_equal(got[-1][0, wild], as_type[wild])
+        assert (np.abs(got[-1][0, ~wild]) <= 1.01 * (np.abs(as_type[~wild]) + np.abs(p.v[0]).max())).all()
