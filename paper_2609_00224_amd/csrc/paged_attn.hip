@@ -52,6 +52,10 @@ struct AttnArgs {
   float* part_ml;    // their maxima and sums
 };
 
+// The first position that a row with `n` positions up to its own sees (n can be
+// negative, and the window as large as the type allows).
+__device__ __forceinline__ int seen_from(const AttnArgs& a, int n) { return a.window > 0 ? max(0, max(0, n) - a.window) : 0; }
+
 // ---------------------------------------------------------------------------
 // Few rows: a task is one sequence, one key/value head and up to 16 R rows
 // (new tokens x the query heads that share the head).  A task's tokens are
@@ -90,7 +94,7 @@ __device__ __forceinline__ SeqWork seq_work(const AttnArgs& a, int s) {
   SeqWork w;
   w.q = load_seq(a.b, s, a.b.max_pages << a.page_shift);
   const int first = w.q.len - w.q.n + 1;  // positions the first row's prefix holds
-  const int lo = a.window > 0 ? max(0, first - a.window) : 0;
+  const int lo = seen_from(a, first);
   w.t0 = lo / kUnit;
   w.cnt = max(1, (w.q.len + kUnit - 1) / kUnit - w.t0);
   w.nqt = (w.q.n * a.group + MT - 1) / MT;
@@ -450,7 +454,7 @@ __global__ __launch_bounds__(kRowThreads, rows_per_cu(DP, FMT, R)) void attn_row
       const int rr = r0 + (ok ? row : 0), i = rr / G, hh = rr - i * G;
       const uint16_t* q = a.q + (token_row0 + i) * a.q_stride + int64_t(h * G + hh) * D;
       hi[r] = ok ? max(0, pos0 + i + 1) : 0;
-      lo[r] = a.window > 0 ? max(0, pos0 + i + 1 - a.window) : 0;
+      lo[r] = seen_from(a, pos0 + i + 1);
 #pragma unroll
       for (int j = 0; j < TL::kSteps; ++j) {
         constexpr int per = TL::kChunk / 8;
@@ -463,8 +467,7 @@ __global__ __launch_bounds__(kRowThreads, rows_per_cu(DP, FMT, R)) void attn_row
     }
     const int i_first = r0 / G, i_last = (r0 + nrow - 1) / G;
     const int hi_min = max(0, pos0 + i_first + 1), hi_max = max(0, pos0 + i_last + 1);
-    const int lo_min = a.window > 0 ? max(0, pos0 + i_first + 1 - a.window) : 0;
-    const int lo_max = a.window > 0 ? max(0, pos0 + i_last + 1 - a.window) : 0;
+    const int lo_min = seen_from(a, pos0 + i_first + 1), lo_max = seen_from(a, pos0 + i_last + 1);
 
     f32x4 o[R][CH];
     float m[R], l[R];
@@ -739,7 +742,7 @@ __global__ __launch_bounds__(kRowThreads, rows_per_cu(DP, FMT, R)) void attn_row
           if (__builtin_expect(s_odd, 0)) {
             // values that are not finite, of the tokens this row sees
             const int i = (r0 + row2) / G;
-            const int to = min(tile_b * kTile, max(0, pos0 + i + 1)), from = a.window > 0 ? max(0, pos0 + i + 1 - a.window) : 0;
+            const int to = min(tile_b * kTile, max(0, pos0 + i + 1)), from = seen_from(a, pos0 + i + 1);
             for (int tok = max(tile_a * kTile, from); tok < to; ++tok) {
               const int tok0 = tok & ~(kTile - 1);
               const int64_t at = tok0 + kTile > hi_min || tok0 < lo_max ? cached_row(a, table, h, tok) : -1;
@@ -873,7 +876,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attn_tile_kernel(
   const int r0 = (nqt - 1 - (task - base)) * kTaskRows, nrow = min(kTaskRows, rows - r0);
   const int pos0 = q.len - q.n;
   auto sees_to = [&](int r) { return max(0, pos0 + r / G + 1); };
-  auto sees_from = [&](int r) { return a.window > 0 ? max(0, pos0 + r / G + 1 - a.window) : 0; };
+  auto sees_from = [&](int r) { return seen_from(a, pos0 + r / G + 1); };
   const int hi_max = sees_to(r0 + nrow - 1), lo_min = sees_from(r0);
   const int hi_min = sees_to(r0), lo_max = sees_from(r0 + nrow - 1);
 

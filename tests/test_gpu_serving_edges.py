@@ -155,3 +155,15 @@ def test_every_scale_and_code_of_a_token_that_one_row_sees(new, qtype, fmt):
         wild = ~np.isfinite(as_type)
         np.testing.assert_array_equal(got[-1][0, wild], as_type[wild])
         assert (np.abs(got[-1][0, ~wild]) <= 1.01 * (np.abs(as_type[~wild]) + np.abs(p.v[0]).max())).all()
+
+
+@pytest.mark.parametrize("new", [5, 90])
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 4, 2 ** 30])
+def test_the_largest_windows_with_more_rows_than_positions(window, new):
+    rng = np.random.default_rng([23, new])
+    p = Paged(rng, [(new - 3, new), (50, 1), (1, new)], 2, 64, 16, "f16")
+    p.qtype = "f16"
+    Q = rounded(rng.standard_normal((p.rows, 8, 64)), "f16")
+    got = _attend(p, Q, window, p.cache())
+    want, bound = attention_reference(p, Q, 0.125)
+    assert (np.abs(got - want) <= bound).all()
