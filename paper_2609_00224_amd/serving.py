@@ -178,7 +178,7 @@ def qtea_paged_attention(cache: KvCache, Q, q_start, kv_len, page_table, out, wo
     """Causal attention of the batch's new tokens, Q [tokens][n_q_heads]
     [head_dim] (fp16 or bf16), over the cache that already holds them, into
     `out` (as Q).  scale: 1 / sqrt(head_dim) unless given; window: positions a
-    row sees, 0 for all."""
+    row sees, 0 for all (a number past the C type's is passed as its largest)."""
     q = _q
     if Q.dim() != 3 or Q.shape != out.shape or Q.dtype != out.dtype:
         raise ValueError("Q and out: one type, one shape [tokens][heads][channels]")
@@ -190,7 +190,7 @@ def qtea_paged_attention(cache: KvCache, Q, q_start, kv_len, page_table, out, wo
     if Q.shape[0] == 0:
         return
     q._check(q.load().qtea_paged_attention(cache.desc, b, Q.data_ptr(), out.data_ptr(), _type(Q, "Q and out"), heads, qs, os_,
-                                           cache.head_dim ** -0.5 if scale is None else scale, window, workspace.data_ptr(),
+                                           cache.head_dim ** -0.5 if scale is None else scale, max(-1, min(window, 0x7fffffff)), workspace.data_ptr(),
                                            workspace.numel() * workspace.element_size(), _stream(stream, cache.device_index)), "qtea_paged_attention")
 
 

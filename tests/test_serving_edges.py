@@ -1,0 +1,55 @@
+"""The serving operators' binding and entry points at the edges of their
+arguments, as far as no device is needed."""
+from __future__ import annotations
+
+import types
+
+import pytest
+import torch
+
+import paper_2609_00224_amd as q
+
+
+class Calls:
+    """Stands for the library: records the calls it gets."""
+
+    def __init__(self):
+        self.made = []
+
+    def __getattr__(self, name):
+        if not name.startswith("qtea_"):
+            raise AttributeError(name)
+        return lambda *args: self.made.append((name, args)) or q.QTEA_OK
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    got = Calls()
+    monkeypatch.setattr(q, "load", lambda: got)
+    return got
+
+
+def _cache(device=-1, heads=2, dim=64):
+    return types.SimpleNamespace(device_index=device, n_heads=heads, head_dim=dim, desc=q.QteaKvCache())
+
+
+def _attend(window=0, stream=types.SimpleNamespace(cuda_stream=0), rows=3, heads=4, dim=64, cache=None):
+    t = torch.zeros((rows, heads, dim), dtype=torch.float16)
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    q.qtea_paged_attention(cache or _cache(), t, i32(3), i32(2), i32(2, 5), t, torch.zeros(64, dtype=torch.uint8), window=window, stream=stream)
+
+
+@pytest.mark.parametrize("window,passed", [(0, 0), (1, 1), (2 ** 31 - 1, 2 ** 31 - 1), (2 ** 31, 2 ** 31 - 1), (2 ** 32, 2 ** 31 - 1), (2 ** 32 + 5, 2 ** 31 - 1),
+                                           (2 ** 63 - 1, 2 ** 31 - 1), (10 ** 30, 2 ** 31 - 1)])
+def test_a_window_past_the_types_range_is_the_largest(calls, window, passed):
+    _attend(window)
+    (name, args), = calls.made
+    assert name == "qtea_paged_attention" and args[9] == passed
+
+
+@pytest.mark.parametrize("window", [-1, -2 ** 31, 5 - 2 ** 32])
+def test_a_negative_window_stays_negative(calls, window):
+    """The entry point refuses it."""
+    _attend(window)
+    (_, args), = calls.made
+    assert args[9] == -1
