@@ -194,8 +194,7 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(const CacheArgs a) {
     } else if constexpr (FMT == QTEA_KV_F16 || FMT == QTEA_KV_BF16) {
       load8<FMT == QTEA_KV_F16 ? QTEA_F16 : QTEA_BF16>(reinterpret_cast<const char*>(codes) + row * (2 * a.dim) + 16 * c, x);
     } else {
-      const uint32_t e = scales[row * (a.dim / 32) + c / 4];
-      const float s = e == 255u ? __builtin_nanf("") : scale_of(e);
+      const float s = scale_value(scales[row * (a.dim / 32) + c / 4]);
       if constexpr (FMT == QTEA_KV_E4M3) {
         const u32x2 v = *reinterpret_cast<const u32x2*>(codes + row * a.dim + 8 * c);
 #pragma unroll

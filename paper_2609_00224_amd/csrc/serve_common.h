@@ -105,8 +105,13 @@ struct BF16 {
   }
 };
 
-// The factor of a scale byte (255: NaN, which the conversions carry on).
+// The factor of a scale byte as the scaled conversions take it: they read its
+// exponent (0 there is 2^-127, 255 a NaN).
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+// The same as a number.
+__device__ __forceinline__ float scale_value(uint32_t byte) {
+  return __uint_as_float(byte == 255u ? 0x7fc00000u : (byte == 0u ? 0x00400000u : byte << 23));
+}
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 

@@ -167,3 +167,34 @@ def test_the_largest_windows_with_more_rows_than_positions(window, new):
     got = _attend(p, Q, window, p.cache())
     want, bound = attention_reference(p, Q, 0.125)
     assert (np.abs(got - want) <= bound).all()
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e2m1"])
+def test_a_scale_byte_of_zero_is_two_to_the_minus_127(fmt):
+    rng = np.random.default_rng(24)
+    p = Paged(rng, [(20, 20)], 2, 64, 16, fmt)
+    cache = p.cache()
+    for t in (cache.k_scale, cache.v_scale):
+        t[int(p.table[0, 0])] = 0
+    k, v = (torch.empty((20, 2, 64), device="cuda") for _ in range(2))
+    q.qtea_kv_read(cache, *p.meta(), k, v)
+    for got, vals, scale in ((k, p.k, p.pool["k"][1]), (v, p.v, p.pool["v"][1])):
+        old = np.repeat(scale.numpy()[p.table[0, 0]].transpose(1, 0, 2).astype(np.float64), 32, -1)
+        want = vals[0].copy()
+        want[:16] *= 2.0 ** -old
+        assert torch.equal(got.cpu().double(), torch.from_numpy(want))
+
+
+@pytest.mark.parametrize("new", [1, 100])
+@pytest.mark.parametrize("fmt,code", [("e4m3", 0x7e), ("e4m3", 0xc8), ("e2m1", 7), ("e2m1", 12)])
+def test_a_scale_byte_of_zero_in_attention(fmt, code, new):
+    """One value everywhere (a normal bf16 one): every average is that value."""
+    rng = np.random.default_rng(25)
+    p = Paged(rng, [(120, new)], 2, 64, 16, fmt)
+    p.qtype = "bf16"
+    cache = p.cache()
+    cache.v.fill_(code if fmt == "e4m3" else code * 17)
+    cache.v_scale.zero_()
+    value = sv.decode(np.full(32, code, np.uint8), np.zeros(1, np.uint8), fmt)[0]
+    got = _attend(p, rounded(rng.standard_normal((new, 8, 64)), "bf16"), 0, cache)
+    assert (np.abs(got / value - 1) <= 1.02 * 2.0 ** -7).all()
