@@ -128,7 +128,8 @@ def _batch(cache, rows, q_start, kv_len, page_table):
 
 
 def _rows(cache, t, heads, what):
-    """A dense operand [tokens][heads][channels]: the stride of its tokens."""
+    """A dense operand [tokens][heads][channels]: the stride of its tokens (of
+    one token it is not used, whatever the view has)."""
     shape, stride, dim = t.shape, t.stride(), cache.head_dim
     if len(shape) != 3 or shape[1] != heads or shape[2] != dim:
         raise ValueError(f"{what}: [tokens][{heads}][{dim}], got {list(shape)}")
@@ -136,7 +137,7 @@ def _rows(cache, t, heads, what):
         raise ValueError(f"{what}: a token's heads and channels are contiguous")
     if t.get_device() != cache.device_index:
         raise ValueError(f"{what}: a tensor of the cache's device")
-    return max(stride[0], heads * dim) if shape[0] <= 1 else stride[0]
+    return heads * dim if shape[0] <= 1 else stride[0]
 
 
 def _dense(name, cache, k, v, q_start, kv_len, page_table, stream):

@@ -198,3 +198,23 @@ def test_a_scale_byte_of_zero_in_attention(fmt, code, new):
     value = sv.decode(np.full(32, code, np.uint8), np.zeros(1, np.uint8), fmt)[0]
     got = _attend(p, rounded(rng.standard_normal((new, 8, 64)), "bf16"), 0, cache)
     assert (np.abs(got / value - 1) <= 1.02 * 2.0 ** -7).all()
+
+
+def test_one_token_of_any_stride():
+    """Of a single token no stride is used: a view with an odd one."""
+    rng = np.random.default_rng(25)
+    p = Paged(rng, [(40, 1)], 2, 64, 16, "f16")
+    p.qtype = "f16"
+    row = lambda x: torch.as_strided(x.reshape(-1), (1, x.shape[1], 64), (1001, 64, 1))  # noqa: E731
+    Q = rounded(rng.standard_normal((1, 8, 64)), "f16")
+    cache, meta = p.cache(), p.meta()
+    k, v = (torch.randn((1, 2, 64), device="cuda").half() for _ in range(2))
+    q.qtea_kv_append(cache, row(k), row(v), *meta)
+    gk, gv = torch.zeros_like(k), torch.zeros_like(v)
+    q.qtea_kv_read(cache, *meta, row(gk), row(gv))
+    assert torch.equal(gk, k) and torch.equal(gv, v)
+    p.k[0][39], p.v[0][39] = k[0].double().cpu().numpy(), v[0].double().cpu().numpy()
+    out = torch.zeros((1, 8, 64), dtype=torch.float16, device="cuda")
+    q.qtea_paged_attention(cache, row(torch.from_numpy(Q).half().cuda()), *meta, row(out), q.new_attention_workspace(8, 64))
+    want, bound = attention_reference(p, Q, 0.125)
+    assert (np.abs(out.double().cpu().numpy() - want) <= bound).all()
