@@ -44,7 +44,7 @@ enum qtea_kv_format {
  *                     16-bit values, E4M3 bytes, or E2M1 pairs (channel 2i
  *                     in the low half of byte i); 16-byte aligned
  *   k_scale, v_scale  device uint8 [n_pages][n_heads][page_size][head_dim/32]
- *                     (quantized formats; NULL otherwise)
+ *                     (quantized formats; NULL otherwise); 16-byte aligned
  *   head_dim          a multiple of 32, 32..256
  *   page_size         a power of two, 16..4096
  *

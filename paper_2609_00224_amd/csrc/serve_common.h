@@ -129,7 +129,7 @@ inline bool cache_ok(const qtea_kv_cache* c) {
   if (c->page_size < 16 || c->page_size > QTEA_KV_MAX_PAGE || (c->page_size & (c->page_size - 1)) != 0) return false;
   if (c->n_pages < 1 || c->n_pages > INT32_MAX) return false;
   if (!aligned16(c->k) || !aligned16(c->v)) return false;
-  if (quantized(c->format) && (!c->k_scale || !c->v_scale)) return false;
+  if (quantized(c->format) && (!c->k_scale || !c->v_scale || !aligned16(c->k_scale) || !aligned16(c->v_scale))) return false;
   return true;
 }
 inline bool batch_ok(const qtea_kv_batch* b, int page_size) {

@@ -2,6 +2,7 @@
 arguments, as far as no device is needed."""
 from __future__ import annotations
 
+import ctypes
 import types
 
 import pytest
@@ -53,3 +54,17 @@ def test_a_negative_window_stays_negative(calls, window):
     _attend(window)
     (_, args), = calls.made
     assert args[9] == -1
+
+
+@pytest.mark.parametrize("which", ["k_scale", "v_scale"])
+@pytest.mark.parametrize("off", [1, 4, 8])
+def test_scale_pools_are_aligned(which, off):
+    """They are read up to 16 bytes at a time."""
+    addr = ctypes.c_void_p(1 << 20)  # never read: every call is refused
+    f = dict(k=1 << 20, v=1 << 20, k_scale=1 << 20, v_scale=1 << 20, n_pages=4, format=2, n_heads=2, head_dim=64, page_size=16)
+    cache = q.QteaKvCache(**{**f, which: (1 << 20) + off})
+    batch = q.QteaKvBatch(q_start=1 << 20, kv_len=1 << 20, page_table=1 << 20, n_tokens=0, n_seq=2, max_pages=5)
+    lib = q.load()
+    for name in ("qtea_kv_append", "qtea_kv_read"):
+        assert getattr(lib, name)(cache, batch, addr, addr, 2, 128, 128, None) == q.QTEA_ERR_INVALID_ARG
+    assert lib.qtea_paged_attention(cache, batch, addr, addr, 0, 8, 512, 512, 0.1, 0, addr, 1 << 40, None) == q.QTEA_ERR_INVALID_ARG
