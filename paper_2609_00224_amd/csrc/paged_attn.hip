@@ -291,7 +291,9 @@ struct Joined {
 
 // Counts this workgroup's arrival; whether it is the last of n.
 __device__ __forceinline__ bool last_to_arrive(uint32_t* counter, int n, int* s_last) {
+  asm volatile("" ::: "memory");  // (no store moves past the wait)
   __builtin_amdgcn_s_waitcnt(0);  // what it stored is complete before its arrival is counted
+  asm volatile("" ::: "memory");
   __syncthreads();
   if (threadIdx.x == 0) {
     const uint32_t before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -362,7 +364,7 @@ constexpr int lds_width(int DP) { return DP < 128 ? DP : 128; }  // channels joi
 constexpr float kMinUnits = 2.0f;  // of a chunk: what joining two costs
 // Workgroups per CU, each of one wave per SIMD: as many as have the registers
 // for a tile on the way beside their sums.
-constexpr int rows_per_cu(int DP, int FMT, int R) { return R * DP >= 256 ? 1 : (FMT == 0 && R * DP == 128 || R == 2 ? 2 : 3); }
+constexpr int rows_per_cu(int DP, int FMT, int R) { return R * DP >= 256 ? 1 : ((FMT == 0 && R * DP == 128) || R == 2 ? 2 : 3); }
 
 // EX: the heads have DP channels; else they have fewer, and what lies past
 // them is read from the first channels instead (queries are 0 there, and sums
