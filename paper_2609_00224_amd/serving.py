@@ -69,6 +69,18 @@ def _stream(stream, device):
     return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
+def _call(name, device, stream, *args):
+    """The entry point on tensors of `device`, which is the current device for
+    the call: a kernel is launched, and its workgroups counted, there."""
+    fn = getattr(_q.load(), name)
+    if torch.cuda.device_count() < 2 or torch.cuda.current_device() == device:
+        rc = fn(*args, _stream(stream, device))
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, _stream(stream, device))
+    _q._check(rc, name)
+
+
 class KvCache:
     """A paged cache's pools: k and v [n_pages][n_heads][page_size][head_dim]
     (fp16 or bf16; uint8 E4M3 codes; uint8 pairs of E2M1 codes, head_dim / 2
@@ -141,14 +153,13 @@ def _rows(cache, t, heads, what):
 
 
 def _dense(name, cache, k, v, q_start, kv_len, page_table, stream):
-    q = _q
     ks, vs = _rows(cache, k, cache.n_heads, "k"), _rows(cache, v, cache.n_heads, "v")
     if k.dtype != v.dtype or k.shape[0] != v.shape[0]:
         raise ValueError("k and v: one type, one number of tokens")
     b = _batch(cache, k.shape[0], q_start, kv_len, page_table)
     if k.shape[0] == 0:
         return
-    q._check(getattr(q.load(), name)(cache.desc, b, k.data_ptr(), v.data_ptr(), _type(k, "k and v"), ks, vs, _stream(stream, cache.device_index)), name)
+    _call(name, cache.device_index, stream, cache.desc, b, k.data_ptr(), v.data_ptr(), _type(k, "k and v"), ks, vs)
 
 
 def qtea_kv_append(cache: KvCache, k, v, q_start, kv_len, page_table, stream=None):
@@ -171,8 +182,9 @@ def qtea_attention_workspace_bytes(n_q_heads: int, head_dim: int) -> int:
 
 
 def new_attention_workspace(n_q_heads: int, head_dim: int, device="cuda"):
-    """A zero-filled workspace for qtea_paged_attention."""
-    return torch.zeros(qtea_attention_workspace_bytes(n_q_heads, head_dim), dtype=torch.uint8, device=device)
+    """A zero-filled workspace for qtea_paged_attention on `device`."""
+    with torch.cuda.device(device):
+        return torch.zeros(qtea_attention_workspace_bytes(n_q_heads, head_dim), dtype=torch.uint8, device=device)
 
 
 def qtea_paged_attention(cache: KvCache, Q, q_start, kv_len, page_table, out, workspace, scale=None, window: int = 0, stream=None):
@@ -180,7 +192,6 @@ def qtea_paged_attention(cache: KvCache, Q, q_start, kv_len, page_table, out, wo
     [head_dim] (fp16 or bf16), over the cache that already holds them, into
     `out` (as Q).  scale: 1 / sqrt(head_dim) unless given; window: positions a
     row sees, 0 for all (a number past the C type's is passed as its largest)."""
-    q = _q
     if Q.dim() != 3 or Q.shape != out.shape or Q.dtype != out.dtype:
         raise ValueError("Q and out: one type, one shape [tokens][heads][channels]")
     heads = Q.shape[1]
@@ -190,9 +201,9 @@ def qtea_paged_attention(cache: KvCache, Q, q_start, kv_len, page_table, out, wo
         raise ValueError("workspace: a contiguous tensor of the cache's device")
     if Q.shape[0] == 0:
         return
-    q._check(q.load().qtea_paged_attention(cache.desc, b, Q.data_ptr(), out.data_ptr(), _type(Q, "Q and out"), heads, qs, os_,
-                                           cache.head_dim ** -0.5 if scale is None else scale, max(-1, min(window, 0x7fffffff)), workspace.data_ptr(),
-                                           workspace.numel() * workspace.element_size(), _stream(stream, cache.device_index)), "qtea_paged_attention")
+    _call("qtea_paged_attention", cache.device_index, stream, cache.desc, b, Q.data_ptr(), out.data_ptr(), _type(Q, "Q and out"), heads, qs, os_,
+          cache.head_dim ** -0.5 if scale is None else scale, max(-1, min(window, 0x7fffffff)), workspace.data_ptr(),
+          workspace.numel() * workspace.element_size())
 
 
 def qtea_verify_workspace_bytes(n_seq: int) -> int:
@@ -214,7 +225,6 @@ def qtea_verify_draft(target, draft, tokens, q_start, u_accept, u_sample, n_acce
     u_accept fp32 [drafts], q_start int32 [n_seq + 1] over the target's rows,
     u_sample fp32 [n_seq]; outputs n_accepted int32 [n_seq] and out_tokens
     int32 [n_seq][max_draft + 1]."""
-    q = _q
     n_seq, n_drafts = u_sample.numel(), tokens.numel()
     if target.dim() != 2 or (target.stride(1) != 1 and target.shape[1] > 1):
         raise ValueError("target: [rows][vocab], a row contiguous")
@@ -237,9 +247,7 @@ def qtea_verify_draft(target, draft, tokens, q_start, u_accept, u_sample, n_acce
     if n_seq == 0:
         return
     one = lambda t: max(t.stride(0), vocab) if t.shape[0] <= 1 else t.stride(0)  # noqa: E731
-    q._check(q.load().qtea_verify_draft(target.data_ptr(), None if draft is None else draft.data_ptr() or None, _type(target, "target"), vocab,
-                                        one(target), 0 if draft is None else one(draft), tokens.data_ptr(), q_start.data_ptr(),
-                                        u_accept.data_ptr(), u_sample.data_ptr(), n_seq, target.shape[0], n_drafts,
-                                        out_tokens.shape[1] - 1, n_accepted.data_ptr(), out_tokens.data_ptr(),
-                                        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream, dev)),
-             "qtea_verify_draft")
+    _call("qtea_verify_draft", dev, stream, target.data_ptr(), None if draft is None else draft.data_ptr() or None, _type(target, "target"), vocab,
+          one(target), 0 if draft is None else one(draft), tokens.data_ptr(), q_start.data_ptr(), u_accept.data_ptr(), u_sample.data_ptr(),
+          n_seq, target.shape[0], n_drafts, out_tokens.shape[1] - 1, n_accepted.data_ptr(), out_tokens.data_ptr(), workspace.data_ptr(),
+          workspace.numel() * workspace.element_size())

@@ -2,6 +2,7 @@
 arguments, as far as no device is needed."""
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import types
 
@@ -68,3 +69,39 @@ def test_scale_pools_are_aligned(which, off):
     for name in ("qtea_kv_append", "qtea_kv_read"):
         assert getattr(lib, name)(cache, batch, addr, addr, 2, 128, 128, None) == q.QTEA_ERR_INVALID_ARG
     assert lib.qtea_paged_attention(cache, batch, addr, addr, 0, 8, 512, 512, 0.1, 0, addr, 1 << 40, None) == q.QTEA_ERR_INVALID_ARG
+
+
+class Devices:
+    """Stands for torch.cuda with two devices, of which 0 is the current one."""
+
+    def __init__(self, monkeypatch):
+        self.current = 0
+        monkeypatch.setattr(torch.cuda, "device_count", lambda: 2)
+        monkeypatch.setattr(torch.cuda, "current_device", lambda: self.current)
+        monkeypatch.setattr(torch.cuda, "device", self.guard)
+
+    @contextlib.contextmanager
+    def guard(self, device):
+        before, self.current = self.current, device
+        yield
+        self.current = before
+
+
+@pytest.mark.parametrize("current", [0, -1])  # (host tensors' device is -1)
+def test_a_call_is_made_on_its_tensors_device(monkeypatch, current):
+    devices, at = Devices(monkeypatch), []
+    devices.current = current
+
+    class On(Calls):
+        def __getattr__(self, name):
+            at.append(devices.current)
+            return lambda *args: at.append(devices.current) or q.QTEA_OK
+
+    monkeypatch.setattr(q, "load", On)
+    stream = types.SimpleNamespace(cuda_stream=0)
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    _attend(stream=stream)
+    t = torch.zeros((3, 2, 64))
+    q.qtea_kv_append(_cache(), t, t, i32(3), i32(2), i32(2, 5), stream=stream)
+    q.qtea_kv_read(_cache(), i32(3), i32(2), i32(2, 5), t, t, stream=stream)
+    assert at[1::2] == [-1] * 3 and devices.current == current
