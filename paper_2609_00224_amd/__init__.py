@@ -21,13 +21,9 @@ qtea_verify_workspace_bytes, qtea_verify_draft.
 from __future__ import annotations
 
 import ctypes
+import importlib
 import os
 from dataclasses import dataclass
-
-from . import serving
-from .serving import (KV_FORMATS, QTEA_BF16, QTEA_F16, QTEA_F32, QTEA_KV_BLOCK, KvCache, QteaKvBatch, QteaKvCache,  # noqa: F401
-                      new_attention_workspace, new_kv_cache, new_verify_workspace, qtea_attention_workspace_bytes,
-                      qtea_kv_append, qtea_kv_read, qtea_paged_attention, qtea_verify_draft, qtea_verify_workspace_bytes)
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libqtea.so")
@@ -65,6 +61,26 @@ QTEA_LAYOUT_FP16 = 2  # residual values fp16
 QTEA_LAYOUT_E4M3 = 3  # residual values FP8 E4M3
 QTEA_LAYOUT_G128 = 4  # 128-column groups with scale and bias, E4M3 residual
 QTEA_GROUPED_MAGIC = 0x51475250
+QTEA_F16, QTEA_BF16, QTEA_F32 = 0, 1, 2
+QTEA_KV_BLOCK = 32
+KV_FORMATS = {"f16": 0, "bf16": 1, "e4m3": 2, "e2m1": 3}
+
+# The serving operators' binding is imported when the first of these is asked
+# for: it needs torch, which the package itself does without.
+_SERVING = ("KvCache", "new_attention_workspace", "new_kv_cache", "new_verify_workspace", "qtea_attention_workspace_bytes",
+            "qtea_kv_append", "qtea_kv_read", "qtea_paged_attention", "qtea_verify_draft", "qtea_verify_workspace_bytes")
+
+
+def __getattr__(name):
+    if name != "serving" and name not in _SERVING:
+        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    serving = importlib.import_module(".serving", __name__)
+    globals().update({n: getattr(serving, n) for n in _SERVING})
+    return globals()[name]
+
+
+def __dir__():
+    return sorted({*globals(), *_SERVING})
 
 
 class QteaDesc(ctypes.Structure):
@@ -96,6 +112,23 @@ class QteaQuantParams(ctypes.Structure):
     _fields_ = [
         ("n_salient", ctypes.c_int64), ("lambda_decay", ctypes.c_double), ("damp", ctypes.c_double),
         ("iters", ctypes.c_int32), ("reserved", ctypes.c_int32),
+    ]
+
+
+class QteaKvCache(ctypes.Structure):
+    """Mirror of struct qtea_kv_cache (include/qtea_serve.h)."""
+    _fields_ = [
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+        ("n_pages", ctypes.c_int64), ("format", ctypes.c_int32), ("n_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32),
+    ]
+
+
+class QteaKvBatch(ctypes.Structure):
+    """Mirror of struct qtea_kv_batch (include/qtea_serve.h)."""
+    _fields_ = [
+        ("q_start", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+        ("n_tokens", ctypes.c_int64), ("n_seq", ctypes.c_int32), ("max_pages", ctypes.c_int32),
     ]
 
 
@@ -176,7 +209,19 @@ def open_library(path: str):
     lib.qtea_quantize.restype = i32
     lib.qtea_quantize.argtypes = [vp, vp, i64, i64, ctypes.POINTER(QteaQuantParams),
                                   vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
-    serving.declare(lib)
+    pc, pb, pi = ctypes.POINTER(QteaKvCache), ctypes.POINTER(QteaKvBatch), ctypes.POINTER(i64)
+    lib.qtea_kv_append.restype = i32
+    lib.qtea_kv_append.argtypes = [pc, pb, vp, vp, i32, i64, i64, vp]
+    lib.qtea_kv_read.restype = i32
+    lib.qtea_kv_read.argtypes = [pc, pb, vp, vp, i32, i64, i64, vp]
+    lib.qtea_attention_workspace_bytes.restype = i32
+    lib.qtea_attention_workspace_bytes.argtypes = [i32, i32, pi]
+    lib.qtea_paged_attention.restype = i32
+    lib.qtea_paged_attention.argtypes = [pc, pb, vp, vp, i32, i32, i64, i64, ctypes.c_float, i32, vp, i64, vp]
+    lib.qtea_verify_workspace_bytes.restype = i32
+    lib.qtea_verify_workspace_bytes.argtypes = [i32, pi]
+    lib.qtea_verify_draft.restype = i32
+    lib.qtea_verify_draft.argtypes = [vp, vp, i32, i64, i64, i64, vp, vp, vp, vp, i32, i64, i64, i32, vp, vp, vp, i64, vp]
     return lib
 
 

@@ -4,7 +4,8 @@ it, and the verification of drafted tokens.
 
 As the rest of the binding, these functions marshal arguments only; every
 step runs in the kernels of ``csrc/kv_cache.hip``, ``csrc/paged_attn.hip`` and
-``csrc/verify.hip``.  They are exported by the package itself.
+``csrc/verify.hip``.  They are exported by the package itself, which imports
+this module when the first of them is asked for.
 """
 from __future__ import annotations
 
@@ -12,45 +13,10 @@ import ctypes
 
 import torch
 
-import paper_2609_00224_amd as _q  # (its functions: this module is imported while it loads)
+import paper_2609_00224_amd as _q
+from paper_2609_00224_amd import KV_FORMATS, QTEA_BF16, QTEA_F16, QTEA_F32, QTEA_KV_BLOCK, QteaKvBatch, QteaKvCache
 
-QTEA_F16, QTEA_BF16, QTEA_F32 = 0, 1, 2
-QTEA_KV_BLOCK = 32
-KV_FORMATS = {"f16": 0, "bf16": 1, "e4m3": 2, "e2m1": 3}
-
-_i64, _i32, _vp = ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p
-
-
-class QteaKvCache(ctypes.Structure):
-    """Mirror of struct qtea_kv_cache (include/qtea_serve.h)."""
-    _fields_ = [
-        ("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("n_pages", _i64),
-        ("format", _i32), ("n_heads", _i32), ("head_dim", _i32), ("page_size", _i32),
-    ]
-
-
-class QteaKvBatch(ctypes.Structure):
-    """Mirror of struct qtea_kv_batch (include/qtea_serve.h)."""
-    _fields_ = [
-        ("q_start", _vp), ("kv_len", _vp), ("page_table", _vp), ("n_tokens", _i64),
-        ("n_seq", _i32), ("max_pages", _i32),
-    ]
-
-
-def declare(lib):
-    """Argument types of the serving entry points of one opened library."""
-    pc, pb, pi = ctypes.POINTER(QteaKvCache), ctypes.POINTER(QteaKvBatch), ctypes.POINTER(_i64)
-    i = ctypes.c_int
-    lib.qtea_kv_append.argtypes = [pc, pb, _vp, _vp, i, _i64, _i64, _vp]
-    lib.qtea_kv_read.argtypes = [pc, pb, _vp, _vp, i, _i64, _i64, _vp]
-    lib.qtea_attention_workspace_bytes.argtypes = [i, i, pi]
-    lib.qtea_paged_attention.argtypes = [pc, pb, _vp, _vp, i, i, _i64, _i64, ctypes.c_float, i, _vp, _i64, _vp]
-    lib.qtea_verify_workspace_bytes.argtypes = [i, pi]
-    lib.qtea_verify_draft.argtypes = [_vp, _vp, i, _i64, _i64, _i64, _vp, _vp, _vp, _vp, i, _i64, _i64, i, _vp, _vp, _vp, _i64, _vp]
-    for name in ("qtea_kv_append", "qtea_kv_read", "qtea_attention_workspace_bytes", "qtea_paged_attention",
-                 "qtea_verify_workspace_bytes", "qtea_verify_draft"):
-        getattr(lib, name).restype = i
-
+_i64 = ctypes.c_int64
 
 _TYPES = {torch.float16: QTEA_F16, torch.bfloat16: QTEA_BF16, torch.float32: QTEA_F32}
 _I32, _F32 = torch.int32, torch.float32

@@ -4,6 +4,9 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import os
+import subprocess
+import sys
 import types
 
 import pytest
@@ -105,3 +108,13 @@ def test_a_call_is_made_on_its_tensors_device(monkeypatch, current):
     q.qtea_kv_append(_cache(), t, t, i32(3), i32(2), i32(2, 5), stream=stream)
     q.qtea_kv_read(_cache(), i32(3), i32(2), i32(2, 5), t, t, stream=stream)
     assert at[1::2] == [-1] * 3 and devices.current == current
+
+
+def test_the_package_and_its_host_entry_points_do_without_torch():
+    """Torch is imported where tensors are, the serving operators' binding with them."""
+    code = ("import sys; sys.modules['torch'] = None\n"
+            "import paper_2609_00224_amd as q\n"
+            "assert q.qtea_abi_version() == q.QTEA_ABI_VERSION and q.qtea_packed_bytes(64, 256, 3) > 0\n"
+            "assert 'KvCache' in dir(q) and q.QteaKvCache and q.KV_FORMATS\n")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    subprocess.run([sys.executable, "-c", code], cwd=root, check=True, timeout=120)
