@@ -147,7 +147,7 @@ int qtea_attention_workspace_bytes(int n_q_heads, int head_dim, int64_t* out_byt
  *              QTEA_BF16; a 16-bit cache's own type), q_stride / out_stride
  *              elements from one token to the next (>= n_q_heads *
  *              head_dim); 16-byte aligned, strides a multiple of 8
- *   scale      > 0 and finite
+ *   scale      > 0, and scale log2(e) an fp32 number (up to 2.3e38)
  *   window     0 (none) or the number of positions a row sees
  *   workspace  device, >= qtea_attention_workspace_bytes
  *

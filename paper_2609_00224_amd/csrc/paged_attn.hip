@@ -23,6 +23,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "serve_common.h"
@@ -1261,7 +1262,8 @@ int qtea_paged_attention(const qtea_kv_cache* cache, const qtea_kv_batch* batch,
   if (q_stride < width || out_stride < width || q_stride % 8 != 0 || out_stride % 8 != 0) return QTEA_ERR_INVALID_ARG;
   if (q_stride > (INT64_MAX >> 34) || out_stride > (INT64_MAX >> 34)) return QTEA_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return QTEA_ERR_INVALID_ARG;
-  if (!(scale > 0.0f) || !(scale <= 3.0e38f) || window < 0) return QTEA_ERR_INVALID_ARG;
+  const float scale_log2 = scale * 1.44269504088896341f;
+  if (!(scale > 0.0f) || !std::isfinite(scale_log2) || window < 0) return QTEA_ERR_INVALID_ARG;
   const int G = n_q_heads / H;
   const int64_t rows = batch->n_tokens * G;
   const int64_t most_units = (int64_t(batch->max_pages) * cache->page_size + kUnit - 1) / kUnit;
@@ -1278,7 +1280,7 @@ int qtea_paged_attention(const qtea_kv_cache* cache, const qtea_kv_batch* batch,
   a.q_stride = q_stride, a.out_stride = out_stride;
   a.b = kernel_batch(batch);
   a.heads = H, a.group = G, a.dim = D, a.page_shift = log2_of(cache->page_size), a.n_pages = int32_t(cache->n_pages), a.window = window;
-  a.scale = scale * 1.44269504088896341f;
+  a.scale = scale_log2;
   a.max_slots = cus * kSlotsPerCu;
   char* ws = static_cast<char*>(workspace);
   a.counters = reinterpret_cast<uint32_t*>(ws);

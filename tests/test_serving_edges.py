@@ -118,3 +118,13 @@ def test_the_package_and_its_host_entry_points_do_without_torch():
             "assert 'KvCache' in dir(q) and q.QteaKvCache and q.KV_FORMATS\n")
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     subprocess.run([sys.executable, "-c", code], cwd=root, check=True, timeout=120)
+
+
+@pytest.mark.parametrize("scale,fits", [(2.3e38, True), (2.4e38, False), (3.0e38, False), (1e-45, True)])
+def test_a_softmax_scale_whose_product_overflows_is_refused(scale, fits):
+    """It would make every score infinite or NaN."""
+    addr = ctypes.c_void_p(1 << 20)  # never read: refused, or no tokens
+    cache = q.QteaKvCache(k=1 << 20, v=1 << 20, n_pages=4, format=0, n_heads=2, head_dim=64, page_size=16)
+    batch = q.QteaKvBatch(q_start=1 << 20, kv_len=1 << 20, page_table=1 << 20, n_tokens=0, n_seq=2, max_pages=5)
+    rc = q.load().qtea_paged_attention(cache, batch, addr, addr, 0, 8, 512, 512, scale, 0, addr, 1 << 40, None)
+    assert (rc != q.QTEA_ERR_INVALID_ARG) == fits
