@@ -36,6 +36,7 @@ enum qtea_kv_format {
 #define QTEA_KV_BLOCK 32       /* channels per scale                       */
 #define QTEA_KV_MAX_DIM 256    /* largest head dimension                   */
 #define QTEA_KV_MAX_PAGE 4096  /* largest page size in tokens              */
+#define QTEA_KV_MAX_LEN (INT32_MAX - 2 * QTEA_KV_MAX_PAGE) /* positions of a page table */
 
 /*
  * A cache: pools of pages, each page page_size tokens of every head.
@@ -78,6 +79,8 @@ typedef struct qtea_kv_cache {
  *   kv_len      device int32 [n_seq], in [0, max_pages * page_size]
  *   page_table  device int32 [n_seq][max_pages]; entries that hold no
  *               position below kv_len are not read as pages
+ *               max_pages * page_size is at most QTEA_KV_MAX_LEN: what the
+ *               kernels add to a position stays an int32
  *   n_tokens    rows of the dense operands; rows outside every sequence
  *               are left as they are
  *

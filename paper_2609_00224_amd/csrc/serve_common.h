@@ -135,7 +135,7 @@ inline bool cache_ok(const qtea_kv_cache* c) {
 inline bool batch_ok(const qtea_kv_batch* b, int page_size) {
   if (!b || !b->q_start || !b->kv_len || !b->page_table) return false;
   if (b->n_seq < 1 || b->max_pages < 1 || b->n_tokens < 0 || b->n_tokens > INT32_MAX) return false;
-  return int64_t(b->max_pages) * page_size <= INT32_MAX;
+  return int64_t(b->max_pages) * page_size <= QTEA_KV_MAX_LEN;
 }
 inline Batch kernel_batch(const qtea_kv_batch* b) {
   return {b->q_start, b->kv_len, b->page_table, int32_t(b->n_tokens), b->n_seq, b->max_pages};

@@ -128,3 +128,17 @@ def test_a_softmax_scale_whose_product_overflows_is_refused(scale, fits):
     batch = q.QteaKvBatch(q_start=1 << 20, kv_len=1 << 20, page_table=1 << 20, n_tokens=0, n_seq=2, max_pages=5)
     rc = q.load().qtea_paged_attention(cache, batch, addr, addr, 0, 8, 512, 512, scale, 0, addr, 1 << 40, None)
     assert (rc != q.QTEA_ERR_INVALID_ARG) == fits
+
+
+@pytest.mark.parametrize("page", [16, 4096])
+def test_the_largest_page_table(page):
+    """Positions and what the kernels add to them are 32-bit numbers."""
+    addr = ctypes.c_void_p(1 << 20)  # never read: refused, or no tokens
+    cache = q.QteaKvCache(k=1 << 20, v=1 << 20, n_pages=4, format=0, n_heads=2, head_dim=64, page_size=page)
+    lib = q.load()
+    for most, fits in (((2 ** 31 - 1 - 8192) // page, True), ((2 ** 31 - 1) // page, False)):
+        batch = q.QteaKvBatch(q_start=1 << 20, kv_len=1 << 20, page_table=1 << 20, n_tokens=0, n_seq=2, max_pages=most)
+        for name in ("qtea_kv_append", "qtea_kv_read"):
+            assert (getattr(lib, name)(cache, batch, addr, addr, 2, 128, 128, None) == q.QTEA_OK) == fits
+        rc = lib.qtea_paged_attention(cache, batch, addr, addr, 0, 8, 512, 512, 0.1, 0, addr, 1 << 40, None)
+        assert (rc != q.QTEA_ERR_INVALID_ARG) == fits
