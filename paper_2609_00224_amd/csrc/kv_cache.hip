@@ -1,8 +1,10 @@
 // The paged cache: writing new tokens' keys and values, quantized on the way,
 // and reading them back.  Both move each byte once; HBM bounds them, and at
-// a few tokens the launch: 32768 fp16 tokens of 8 x 128 channels into E4M3
-// 33 us (143 MB at 4.3 TB/s; a large copy reaches 4.8), 60000 read from it into
-// fp16 58 us (252 MB, 4.4 TB/s), 16 tokens 3.0 us.
+// a few tokens the launch: 23034 fp16 tokens of 8 x 128 channels into E4M3
+// 33 us (143 MB at 4.3 TB/s; a large copy reaches 4.6 to 4.8), 40533 read from
+// it into fp16 58 us (252 MB, 4.4 TB/s), 16 tokens 3.6 us.  (Passes over several
+// caches in turn; over one alone its codes stay in the Infinity Cache, and the
+// same read takes 43.)
 //
 // A block's scale is a power of two, so the division by it and (within the
 // exponents written) every decoded value are exact: the only rounding is the

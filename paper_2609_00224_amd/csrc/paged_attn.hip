@@ -19,7 +19,9 @@
 // them in registers from the load to the product; beyond, the products do,
 // and attn_tile_kernel shares tiles in LDS among 128 rows.  On both sides of the
 // line (16 sequences, nine tokens of five query heads a group on average, up
-// to 9000 bf16 positions): 89 us against 195.
+// to 9000 bf16 positions): 89 us against 195.  The choice is the call's: single
+// tokens beside a long chunk go to the second kernel with it, whose workgroups
+// are few for them.
 #include <math.h>
 
 #include <algorithm>
@@ -74,8 +76,9 @@ __device__ __forceinline__ int seen_from(const AttnArgs& a, int n) { return a.wi
 //
 // Bound by HBM for long histories (one token over 260001 positions in E2M1,
 // 283 MB: 61 us; 16 tokens over up to 16000 in E4M3, 360 MB: 73 us; each
-// further position at 6.0 to 6.3 TB/s), below that by the chain of dependent
-// reads: lengths, pages, values, parts (one token over 700: 10.4 us, of which
+// further byte at 5.7 to 6.6 TB/s, of 7.1 that a plain read reaches, beside 15
+// to 18 us for the start and the join), below that by the chain of dependent
+// reads: lengths, pages, values, parts (one token over 700: 10.5 us, of which
 // 1.1 are the launch, 1.5 the chunk search, 1.1 the pages, 2 the one tile, 0.9
 // the waves' join, 3 the arrival and the parts).  A wave of 32 rows reads
 // each value once, which is faster than two waves of 16 that read it from the
@@ -804,11 +807,12 @@ __global__ __launch_bounds__(kRowThreads, rows_per_cu(DP, FMT, R)) void attn_row
 // Bound by instruction issue: for 64 tokens x 32 rows x 128 channels a wave
 // issues 32 products (1024 cycles of its SIMD) and about 265 vector
 // instructions (1440 cycles, of them 512 for the exponentials), and the two
-// waves of a SIMD overlap little of the one with the other: 37 % of the
-// cycles have a product in the matrix core, 47 % a vector instruction.  A
-// 2048-token chunk over 12345 positions, 32 heads, E4M3: 440 us, 864 TFLOP/s
-// (fp16 cache 816, E2M1 902); six prompts of up to 4000 tokens, 64 channels,
-// window 1024, bf16: 108 us, 594 TFLOP/s of the pairs in the windows.
+// waves of a SIMD overlap little of the one with the other: 38 % of the
+// cycles have a product in the matrix core, 49 % a vector instruction.  A
+// 2048-token chunk over 12345 positions, 32 heads, E4M3: 430 us, 883 TFLOP/s
+// (fp16 cache 831, E2M1 917); six prompts of up to 4000 tokens, 64 channels,
+// window 1024, bf16: 107 us, 605 TFLOP/s of the pairs in the windows (28 and
+// 66 % of the cycles).
 // ---------------------------------------------------------------------------
 constexpr int kTaskRows = 128;
 constexpr int kMinPart = 4;   // tiles of a part, at least
