@@ -42,7 +42,7 @@
 extern "C" {
 #endif
 
-#define QTEA_ABI_VERSION 10
+#define QTEA_ABI_VERSION 11
 #define QTEA_MAX_BATCH 16
 
 enum qtea_status {
@@ -53,7 +53,8 @@ enum qtea_status {
                                 a salient bitmap that disagrees with n_salient
                                 or marks a column >= K, an E4M3 NaN value,
                                 an fp16 residual value that is not finite */
-  QTEA_ERR_BATCH = -4,       /* batch outside [1, QTEA_MAX_BATCH]            */
+  QTEA_ERR_BATCH = -4,       /* batch outside [1, QTEA_MAX_BATCH], or
+                                [1, QTEA_W4_MAX_BATCH] (qtea_layer.h)        */
   QTEA_ERR_WORKSPACE = -5,   /* workspace or packed buffer too small         */
   QTEA_ERR_HIP = -6,         /* a HIP runtime call or kernel launch failed   */
   QTEA_ERR_NOT_POSITIVE = -7,/* a Hessian that is not positive definite

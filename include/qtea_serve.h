@@ -1,8 +1,9 @@
 /*
  * qtea_serve.h - C ABI of the operators that stand around the compressed
  * products in a decoder's serving step, for MI355X (gfx950): a paged
- * key/value cache in 16, 8 or 4 bits, causal attention of a batch's newest
- * tokens over it, and the verification of drafted tokens.
+ * key/value cache in 16, 8 or 4 bits with the rotation of keys and queries by
+ * their positions, causal attention of a batch's newest tokens over it, and the
+ * verification of drafted tokens.
  *
  * Conventions as in qtea.h: plain C, device pointers owned by the caller,
  * nothing is allocated, device work is enqueued on `stream` and never
@@ -115,6 +116,38 @@ typedef struct qtea_kv_batch {
  */
 int qtea_kv_append(const qtea_kv_cache* cache, const qtea_kv_batch* batch, const void* k, const void* v, int type,
                    int64_t k_stride, int64_t v_stride, void* stream);
+
+/*
+ * qtea_kv_append with the rotation by position: query and key heads are
+ * rotated by their tokens' positions, the queries go to q_out, the keys and
+ * (as they are) the values into the cache.  For a token at position p, pair i
+ * of a head's first rot_dim channels (i < rot_dim / 2) turns by p * freq[i]:
+ *
+ *   (a, b) <- (a cos - b sin, b cos + a sin),
+ *
+ * pair i being channels i and i + rot_dim / 2, or, interleaved, 2i and 2i + 1.
+ * The angle is taken in 64 bits, its sine and cosine and the products in 32;
+ * then one rounding, to q_out_type or the cache's format.
+ *
+ *   q, k, v     device [n_tokens][n_q_heads (q) or n_heads][head_dim] of
+ *               `type`, strides and alignment as qtea_kv_append's: the three
+ *               parts of a fused projection's output can be passed in place
+ *   q_out       device [n_tokens][n_q_heads][head_dim] of q_out_type (enum
+ *               qtea_type), q_out_stride elements from token to token; 16-byte
+ *               aligned, stride a multiple of 16 bytes.  It may be q itself
+ *               (same type and stride); other operands must not overlap it
+ *   n_q_heads   0 .. 65535; 0: keys and values only (q and q_out NULL)
+ *   freq        device fp32 [rot_dim / 2], of magnitude up to 2^20
+ *   rot_dim     a multiple of 16, 16 .. head_dim; channels past it are
+ *               not turned
+ * A token whose position is negative (n_s > kv_len[s]) gets a q_out of zeros, one
+ * of a sequence whose kv_len is out of range NaN; rows of no sequence are
+ * left as they are.
+ * Errors: QTEA_ERR_INVALID_ARG, QTEA_ERR_HIP.
+ */
+int qtea_kv_append_rotated(const qtea_kv_cache* cache, const qtea_kv_batch* batch, const void* q, const void* k, const void* v,
+                           int type, int64_t q_stride, int64_t k_stride, int64_t v_stride, int n_q_heads, const float* freq,
+                           int rot_dim, int interleaved, void* q_out, int q_out_type, int64_t q_out_stride, void* stream);
 
 /*
  * Read the batch's rows back: the inverse of qtea_kv_append, with the same

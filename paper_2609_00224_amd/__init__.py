@@ -5,8 +5,9 @@ kernels of ``csrc/qtea.hip``, ``csrc/grouped.hip``, ``csrc/grouped_mma.hip``,
 ``csrc/tern_mfma.hip`` and ``csrc/tern_solo.hip`` behind the C ABI of ``include/qtea.h``, and every step of the offline
 quantizer in those of ``csrc/quant.hip`` behind ``include/qtea_quant.h``.  The
 serving operators around the products (paged cache, attention, draft
-verification; ``include/qtea_serve.h``) are bound in ``serving.py``.  Torch
-is used to allocate device memory and to name the current HIP stream.
+verification; ``include/qtea_serve.h``) are bound in ``serving.py``, those of a
+decoder layer (norm, gated activation, products with 4-bit weights;
+``include/qtea_layer.h``) in ``layer.py``.  Torch is used to allocate device memory and to name the current HIP stream.
 There is no CPU fallback: if the library is not built, loading it raises.
 
 Entry points carry the C names: qtea_packed_bytes, qtea_pack,
@@ -16,7 +17,9 @@ qtea_debug_unpack, qtea_read_ceiling, qtea_status_string, qtea_abi_version,
 qtea_grouped_plan_bytes, qtea_grouped_plan, qtea_grouped_gemv, qtea_grouped_status,
 qtea_quant_hessian, qtea_quant_workspace_bytes, qtea_quantize, qtea_kv_append,
 qtea_kv_read, qtea_attention_workspace_bytes, qtea_paged_attention,
-qtea_verify_workspace_bytes, qtea_verify_draft.
+qtea_verify_workspace_bytes, qtea_verify_draft, qtea_kv_append_rotated,
+qtea_rms_norm, qtea_silu_mul, qtea_w4_packed_bytes, qtea_w4_pack,
+qtea_w4_unpack, qtea_w4_gemm_lowbatch.
 """
 from __future__ import annotations
 
@@ -43,7 +46,7 @@ QTEA_ERR_HIP = -6
 QTEA_ERR_NOT_POSITIVE = -7
 QTEA_QUANT_GROUP = 128
 QTEA_MAX_BATCH = 16
-QTEA_ABI_VERSION = 10  # the header this binding mirrors
+QTEA_ABI_VERSION = 11  # the header this binding mirrors
 QTEA_DESC_MAGIC = 0x51544541
 
 # Every function the header declares (checked by tests/test_abi.py).
@@ -55,32 +58,39 @@ EXPORTS = (
     "qtea_packed_bytes_e4m3", "qtea_pack_e4m3", "qtea_packed_bytes_g128", "qtea_pack_g128",
     "qtea_read_ceiling", "qtea_quant_hessian", "qtea_quant_workspace_bytes", "qtea_quantize",
     "qtea_kv_append", "qtea_kv_read", "qtea_attention_workspace_bytes", "qtea_paged_attention",
-    "qtea_verify_workspace_bytes", "qtea_verify_draft",
+    "qtea_verify_workspace_bytes", "qtea_verify_draft", "qtea_kv_append_rotated",
+    "qtea_rms_norm", "qtea_silu_mul", "qtea_w4_packed_bytes", "qtea_w4_pack", "qtea_w4_unpack", "qtea_w4_gemm_lowbatch",
 )
 QTEA_LAYOUT_FP16 = 2  # residual values fp16
 QTEA_LAYOUT_E4M3 = 3  # residual values FP8 E4M3
 QTEA_LAYOUT_G128 = 4  # 128-column groups with scale and bias, E4M3 residual
 QTEA_GROUPED_MAGIC = 0x51475250
 QTEA_F16, QTEA_BF16, QTEA_F32 = 0, 1, 2
+QTEA_E4M3 = 3  # beside the three: codes with a scale per block of 32 (include/qtea_layer.h)
 QTEA_KV_BLOCK = 32
+QTEA_NORM_MAX_DIM = 65536
+QTEA_W4_MAX_BATCH = 64
 KV_FORMATS = {"f16": 0, "bf16": 1, "e4m3": 2, "e2m1": 3}
 
-# The serving operators' binding is imported when the first of these is asked
-# for: it needs torch, which the package itself does without.
+# The bindings of the serving and layer operators are imported when the first
+# of these is asked for: they need torch, which the package itself does without.
 _SERVING = ("KvCache", "new_attention_workspace", "new_kv_cache", "new_verify_workspace", "qtea_attention_workspace_bytes",
-            "qtea_kv_append", "qtea_kv_read", "qtea_paged_attention", "qtea_verify_draft", "qtea_verify_workspace_bytes")
+            "qtea_kv_append", "qtea_kv_append_rotated", "qtea_kv_read", "qtea_paged_attention", "qtea_verify_draft", "qtea_verify_workspace_bytes")
+_LAYER = ("W4Matrix", "pack_matrix_w4", "qtea_rms_norm", "qtea_silu_mul", "qtea_w4_gemm_lowbatch", "qtea_w4_pack", "qtea_w4_packed_bytes",
+          "qtea_w4_unpack")
 
 
 def __getattr__(name):
-    if name != "serving" and name not in _SERVING:
-        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
-    serving = importlib.import_module(".serving", __name__)
-    globals().update({n: getattr(serving, n) for n in _SERVING})
-    return globals()[name]
+    for module, names in (("serving", _SERVING), ("layer", _LAYER)):
+        if name == module or name in names:
+            m = importlib.import_module("." + module, __name__)
+            globals().update({n: getattr(m, n) for n in names})
+            return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
 
 
 def __dir__():
-    return sorted({*globals(), *_SERVING})
+    return sorted({*globals(), *_SERVING, *_LAYER})
 
 
 class QteaDesc(ctypes.Structure):
@@ -212,6 +222,8 @@ def open_library(path: str):
     pc, pb, pi = ctypes.POINTER(QteaKvCache), ctypes.POINTER(QteaKvBatch), ctypes.POINTER(i64)
     lib.qtea_kv_append.restype = i32
     lib.qtea_kv_append.argtypes = [pc, pb, vp, vp, i32, i64, i64, vp]
+    lib.qtea_kv_append_rotated.restype = i32
+    lib.qtea_kv_append_rotated.argtypes = [pc, pb, vp, vp, vp, i32, i64, i64, i64, i32, vp, i32, i32, vp, i32, i64, vp]
     lib.qtea_kv_read.restype = i32
     lib.qtea_kv_read.argtypes = [pc, pb, vp, vp, i32, i64, i64, vp]
     lib.qtea_attention_workspace_bytes.restype = i32
@@ -222,6 +234,18 @@ def open_library(path: str):
     lib.qtea_verify_workspace_bytes.argtypes = [i32, pi]
     lib.qtea_verify_draft.restype = i32
     lib.qtea_verify_draft.argtypes = [vp, vp, i32, i64, i64, i64, vp, vp, vp, vp, i32, i64, i64, i32, vp, vp, vp, i64, vp]
+    lib.qtea_rms_norm.restype = i32
+    lib.qtea_rms_norm.argtypes = [vp, i32, i64, vp, i32, i64, vp, i32, ctypes.c_float, vp, i32, i64, vp, i64, i64, i32, i64, vp]
+    lib.qtea_silu_mul.restype = i32
+    lib.qtea_silu_mul.argtypes = [vp, vp, i32, i64, i64, vp, i32, i64, vp, i64, i64, i64, vp]
+    lib.qtea_w4_packed_bytes.restype = i32
+    lib.qtea_w4_packed_bytes.argtypes = [i64, i64, pi]
+    lib.qtea_w4_pack.restype = i32
+    lib.qtea_w4_pack.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp]
+    lib.qtea_w4_unpack.restype = i32
+    lib.qtea_w4_unpack.argtypes = [vp, i64, i64, i64, vp, i32, i64, vp]
+    lib.qtea_w4_gemm_lowbatch.restype = i32
+    lib.qtea_w4_gemm_lowbatch.argtypes = [vp, i64, i64, i64, vp, i32, i64, vp, i64, i32, vp, i32, i64, vp]
     return lib
 
 

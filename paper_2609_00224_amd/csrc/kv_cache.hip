@@ -15,9 +15,10 @@
 // sequences' starts while the row's values are already on their way.  A lane
 // holds 8 channels, so a block of 32 channels is a quad of lanes and its
 // largest magnitude two DPP steps away.
+#include <algorithm>
 #include <type_traits>
 
-#include "serve_common.h"
+#include "rows.h"
 
 namespace qtea_serve {
 namespace {
@@ -35,8 +36,8 @@ struct CacheArgs {
 
 // Where row r is cached: its page and offset in it.
 struct Place {
-  int page, off;
-  bool some, bad;  // whether it has a position, and whether that has no page
+  int page, off, pos;
+  bool some, bad, bad_len;  // whether it is in a sequence, whether it has no page, and that for its sequence's length
 };
 
 __device__ __forceinline__ Place place_of(const CacheArgs& a, int r) {
@@ -48,16 +49,16 @@ __device__ __forceinline__ Place place_of(const CacheArgs& a, int r) {
     const int s = s0 + lane;
     before += __popcll(__ballot(s < a.b.n_seq && a.b.q_start[min(s, a.b.n_seq - 1)] <= r));
   }
-  Place p = {0, 0, false, false};
+  Place p = {0, 0, 0, false, false, false};
   if (before == 0) return p;
   const int s = __builtin_amdgcn_readfirstlane(before - 1);
   const int cap = a.b.max_pages << a.page_shift;
   const Seq q = load_seq(a.b, s, cap);
   if (r < q.first || r >= q.first + q.n) return p;
   p.some = true;
-  p.bad = q.bad;
+  p.bad = p.bad_len = q.bad;
   if (q.bad) return p;
-  const int pos = q.len - q.n + (r - q.first);
+  const int pos = p.pos = q.len - q.n + (r - q.first);
   if (pos < 0) {
     p.off = -1;
     return p;
@@ -68,53 +69,20 @@ __device__ __forceinline__ Place place_of(const CacheArgs& a, int r) {
   return p;
 }
 
-// 8 values of a dense row.
-template <int TYPE>
-__device__ __forceinline__ void load8(const char* p, float (&x)[8]) {
-  if constexpr (TYPE == QTEA_F32) {
-    const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 16);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
-  } else if constexpr (TYPE == QTEA_F16) {
-    const half8_t v = *reinterpret_cast<const half8_t*>(p);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = float(v[i]);
-  } else {
-    const u32x4 v = *reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(v[i] << 16), x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
-  }
-}
-template <int TYPE>
-__device__ __forceinline__ void store8(char* p, const float (&x)[8]) {
-  if constexpr (TYPE == QTEA_F32) {
-    *reinterpret_cast<f32x4*>(p) = f32x4{x[0], x[1], x[2], x[3]};
-    *reinterpret_cast<f32x4*>(p + 16) = f32x4{x[4], x[5], x[6], x[7]};
-  } else {
-    u32x4 v;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = TYPE == QTEA_F16 ? F16::pack(x[2 * i], x[2 * i + 1]) : BF16::pack(x[2 * i], x[2 * i + 1]);
-    *reinterpret_cast<u32x4*>(p) = v;
-  }
-}
-
-__device__ __forceinline__ uint32_t quad_max(uint32_t x) {
-  const uint32_t y = max(x, uint32_t(__builtin_amdgcn_update_dpp(0, int(x), 0xB1, 0xf, 0xf, true)));  // 1,0,3,2
-  return max(y, uint32_t(__builtin_amdgcn_update_dpp(0, int(y), 0x4E, 0xf, 0xf, true)));              // 2,3,0,1
-}
-
-// Biased exponent of a block's scale: the smallest power of two under which
-// its largest magnitude `amax` (bits of an fp32) is at most the format's
-// largest code, 1.75 * 2^8 or 1.5 * 2^2; within the range for which every
-// code times it is an fp16 value.  Not finite: 255.
+// Writes one lane's 8 channels c * 8 .. of a cached row, the quad's lanes
+// together (they hold a block).
 template <int FMT>
-__device__ __forceinline__ uint32_t block_exponent(uint32_t amax) {
-  if (amax >= 0x7f800000u) return 255u;
-  constexpr int above = FMT == QTEA_KV_E4M3 ? 8 : 2;
-  constexpr uint32_t top = FMT == QTEA_KV_E4M3 ? 0x600000u : 0x400000u;
-  constexpr int low = FMT == QTEA_KV_E4M3 ? 127 - 15 : 127 - 23, high = FMT == QTEA_KV_E4M3 ? 127 + 7 : 127 + 13;
-  const int e = int(amax >> 23) - above + ((amax & 0x7fffffu) > top ? 1 : 0);
-  return uint32_t(min(max(e, low), high));
+__device__ __forceinline__ void store_cached(const CacheArgs& a, int kv, int64_t row, int c, float (&x)[8]) {
+  uint8_t* codes = kv ? a.codes[1] : a.codes[0];
+  if constexpr (FMT == QTEA_KV_F16 || FMT == QTEA_KV_BF16) {
+    store8<FMT == QTEA_KV_F16 ? QTEA_F16 : QTEA_BF16>(reinterpret_cast<char*>(codes) + row * (2 * a.dim) + 16 * c, x);
+  } else {
+    const uint32_t e = block_exponent<FMT>(quad_max(max_bits(x)));
+    const u32x2 v = block_codes<FMT>(x, e);
+    if constexpr (FMT == QTEA_KV_E4M3) *reinterpret_cast<u32x2*>(codes + row * a.dim + 8 * c) = v;
+    else *reinterpret_cast<uint32_t*>(codes + row * (a.dim / 2) + 4 * c) = v[0];
+    if ((c & 3) == 0) (kv ? a.scales[1] : a.scales[0])[row * (a.dim / 32) + c / 4] = uint8_t(e);
+  }
 }
 
 template <int FMT, int TYPE>
@@ -130,43 +98,127 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(const CacheArgs a) 
   if (lane < octs) load8<TYPE>(src + lane * (8 * kSize), x);
   const Place p = place_of(a, r);
   if (!p.some || p.bad || p.off < 0) return;
-  uint8_t* codes = kv ? a.codes[1] : a.codes[0];
-  uint8_t* scales = kv ? a.scales[1] : a.scales[0];
   const int64_t row0 = (int64_t(p.page) * a.heads << a.page_shift) + p.off;  // row of head 0; heads a page apart
   for (int o = lane; o < octs; o += 64) {
     if (o != lane) load8<TYPE>(src + o * (8 * kSize), x);
     const int h = o / per, c = o - h * per;
-    const int64_t row = row0 + (int64_t(h) << a.page_shift);
-    if constexpr (FMT == QTEA_KV_F16 || FMT == QTEA_KV_BF16) {
-      store8<FMT == QTEA_KV_F16 ? QTEA_F16 : QTEA_BF16>(reinterpret_cast<char*>(codes) + row * (2 * a.dim) + 16 * c, x);
-    } else {
-      // (a quad's lanes are together in or out: heads * dim / 8 is a multiple of 4)
-      uint32_t m = 0;
+    // (a quad's lanes are together in or out: heads * dim / 8 is a multiple of 4)
+    store_cached<FMT>(a, kv, row0 + (int64_t(h) << a.page_shift), c, x);
+  }
+}
+
+// Keys and queries turned by their positions on the way.  A wave takes a run of
+// one token's tasks, a task as many whole heads as it has room for at 8 channels
+// a lane, so that a lane's channels are the same in every task: it keeps their
+// sines and cosines, which the wave finds once, an angle a lane, and passes
+// round through LDS.  The other half of a pair that is rot_dim / 2 channels away is
+// loaded a second time (it is in the L1).
+//
+// An angle is a product of a position (31 bits) and a frequency (24), in double with
+// what its rounding left, less the nearest multiple of pi / 2 in two doubles:
+// what is left is at most pi / 4 and exact to fp32's last bits.
+struct RotateArgs {
+  CacheArgs c;
+  const char* q;
+  char* q_out;
+  int64_t q_stride, q_out_stride;  // bytes
+  const float* freq;
+  int32_t q_heads, rot, interleaved, q_out_type;
+  int32_t tasks, parts, per_part;  // tasks of a token, waves that share them, tasks a wave
+};
+
+constexpr int kMaxAngles = QTEA_KV_MAX_DIM / 2;
+
+__device__ __forceinline__ void turn_of(int pos, float freq, float& cs, float& sn) {
+  const double p = double(pos), f = double(freq), angle = p * f, rest = __builtin_fma(p, f, -angle);
+  const double n = __builtin_rint(angle * 0x1.45f306dc9c883p-1);  // 2 / pi
+  // pi / 2 to 106 bits
+  double r = __builtin_fma(n, -0x1.921fb54442d18p+0, angle);
+  r = __builtin_fma(n, -0x1.1a62633145c07p-54, r) + rest;
+  const float x = float(r), s = sinf(x), c = cosf(x);
+  const int quarter = int(int64_t(n) & 3);
+  sn = quarter & 1 ? c : s;
+  cs = quarter & 1 ? s : c;
+  if (quarter & 2) sn = -sn;
+  if (quarter == 1 || quarter == 2) cs = -cs;
+}
+
+template <int FMT, int TYPE>
+__global__ __launch_bounds__(kThreads) void kv_append_rotated_kernel(const RotateArgs a) {
+  __shared__ float s_turn[kThreads / 64][2][kMaxAngles];
+  const CacheArgs& ca = a.c;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int kSize = TYPE == QTEA_F32 ? 4 : 2;
+  const int per = ca.dim / 8, heads = 64 / per;  // lanes of a head, heads of a task
+  const int hl = lane / per, c = lane - hl * per;
+  const int nq = (a.q_heads + heads - 1) / heads, nkv = (ca.heads + heads - 1) / heads;
+  const int half = a.rot / 2, h8 = a.rot / 16;
+  const bool turned = 8 * c < a.rot;
+  const int other = c < h8 ? h8 : -h8;  // octs to the pairs' other halves
+  const int64_t waves = int64_t(ca.b.n_tokens) * a.parts;
+  for (int64_t w0 = int64_t(blockIdx.x) * (kThreads / 64); w0 < waves; w0 += int64_t(gridDim.x) * (kThreads / 64)) {
+    const int w = __builtin_amdgcn_readfirstlane(int(w0) + wave);
+    const int r = w / a.parts, part = w - r * a.parts;
+    if (r >= ca.b.n_tokens) return;
+    const int first = part * a.per_part, last = min(first + a.per_part, a.tasks);
+    const Place p = place_of(ca, r);
+    if (!p.some) continue;
+    const bool none = p.bad_len || p.pos < 0;
+    float cs[8], sn[8];
+    if (!none && first < nq + nkv) {
+      for (int i = lane; i < half; i += 64) turn_of(p.pos, a.freq[i], s_turn[wave][0][i], s_turn[wave][1][i]);
+      // (a wave's LDS accesses are made in order; only the compiler has to keep it)
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      const int base = a.interleaved ? 4 * c : (c < h8 ? 8 * c : 8 * c - half);
+      if (turned) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
-      const uint32_t e = block_exponent<FMT>(quad_max(m));
-      const bool nan = e == 255u;
-      const float inv = __uint_as_float((254u - (nan ? 127u : e)) << 23);  // exact: a power of two
-      constexpr float top = FMT == QTEA_KV_E4M3 ? 448.0f : 6.0f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_fmed3f(x[i] * inv, -top, top);
-      if constexpr (FMT == QTEA_KV_E4M3) {
-        u32x2 v;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          int q = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i], x[4 * i + 1], 0, false);
-          q = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 2], x[4 * i + 3], q, true);
-          v[i] = nan ? 0x7f7f7f7fu : uint32_t(q);
+        for (int i = 0; i < 8; ++i) {
+          const int at = base + (a.interleaved ? i / 2 : i);
+          cs[i] = s_turn[wave][0][at], sn[i] = s_turn[wave][1][at];
         }
-        *reinterpret_cast<u32x2*>(codes + row * a.dim + 8 * c) = v;
-      } else {
-        uint32_t v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, x[0], x[1], 1.0f, 0);
-        v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, x[2], x[3], 1.0f, 1);
-        v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, x[4], x[5], 1.0f, 2);
-        v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, x[6], x[7], 1.0f, 3);
-        *reinterpret_cast<uint32_t*>(codes + row * (a.dim / 2) + 4 * c) = nan ? 0u : v;
       }
-      if ((lane & 3) == 0) scales[row * (a.dim / 32) + c / 4] = uint8_t(e);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+    const int64_t row0 = (int64_t(p.bad ? 0 : p.page) * ca.heads << ca.page_shift) + max(p.off, 0);
+    for (int t = first; t < last; ++t) {
+      const int seg = t < nq ? 0 : (t < nq + nkv ? 1 : 2);  // queries, keys, values
+      const int head = (t - (seg == 0 ? 0 : (seg == 1 ? nq : nq + nkv))) * heads + hl;
+      if (hl >= heads || head >= (seg == 0 ? a.q_heads : ca.heads)) continue;
+      if (seg != 0 && (none || p.bad)) continue;
+      float x[8];
+      if (none) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = p.bad_len ? __builtin_nanf("") : 0.0f;
+      } else {
+        const char* src = seg == 0 ? a.q + int64_t(r) * a.q_stride : ca.dense[seg - 1] + int64_t(r) * ca.stride[seg - 1];
+        src += (int64_t(head) * ca.dim + 8 * c) * kSize;
+        load8<TYPE>(src, x);
+        if (turned && seg != 2) {
+          float y[8];
+          if (a.interleaved) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = x[i ^ 1];
+          } else {
+            load8<TYPE>(src + other * 8 * kSize, y);
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const bool low = a.interleaved ? (i & 1) == 0 : c < h8;
+            x[i] = x[i] * cs[i] + (low ? -y[i] : y[i]) * sn[i];
+          }
+        }
+      }
+      if (seg == 0) {
+        char* dst = a.q_out + int64_t(r) * a.q_out_stride;
+        const int64_t at = int64_t(head) * ca.dim + 8 * c;
+        if (a.q_out_type == QTEA_F16) store8<QTEA_F16>(dst + at * 2, x);
+        else if (a.q_out_type == QTEA_BF16) store8<QTEA_BF16>(dst + at * 2, x);
+        else store8<QTEA_F32>(dst + at * 4, x);
+      } else {
+        store_cached<FMT>(ca, seg - 1, row0 + (int64_t(head) << ca.page_shift), c, x);
+      }
     }
   }
 }
@@ -265,6 +317,36 @@ int qtea_kv_append(const qtea_kv_cache* cache, const qtea_kv_batch* batch, const
   for_kernel(cache->format, type, [&](auto fmt, auto ty) {
     hipLaunchKernelGGL((kv_append_kernel<decltype(fmt)::value, decltype(ty)::value>), dim3(row_blocks(a.b.n_tokens)),
                        dim3(kThreads), 0, static_cast<hipStream_t>(stream), a);
+  });
+  return hipGetLastError() == hipSuccess ? QTEA_OK : QTEA_ERR_HIP;
+}
+
+int qtea_kv_append_rotated(const qtea_kv_cache* cache, const qtea_kv_batch* batch, const void* q, const void* k, const void* v,
+                           int type, int64_t q_stride, int64_t k_stride, int64_t v_stride, int n_q_heads, const float* freq,
+                           int rot_dim, int interleaved, void* q_out, int q_out_type, int64_t q_out_stride, void* stream) {
+  RotateArgs a;
+  if (!cache_args(cache, batch, k, v, type, k_stride, v_stride, &a.c)) return QTEA_ERR_INVALID_ARG;
+  if (n_q_heads < 0 || n_q_heads > 65535 || !freq || (reinterpret_cast<uintptr_t>(freq) & 3) != 0) return QTEA_ERR_INVALID_ARG;
+  if (rot_dim < 16 || rot_dim > cache->head_dim || rot_dim % 16 != 0 || q_out_type < QTEA_F16 || q_out_type > QTEA_F32) return QTEA_ERR_INVALID_ARG;
+  if (n_q_heads > 0) {
+    const int64_t width = int64_t(n_q_heads) * cache->head_dim;
+    if (!q || !q_out || !stride_ok(q_stride, width) || !stride_ok(q_out_stride, width)) return QTEA_ERR_INVALID_ARG;
+    if (!rows_aligned16(q, q_stride, type) || !rows_aligned16(q_out, q_out_stride, q_out_type)) return QTEA_ERR_INVALID_ARG;
+    if (q == q_out && (type != q_out_type || q_stride != q_out_stride)) return QTEA_ERR_INVALID_ARG;
+  } else {
+    q_stride = q_out_stride = 0;
+  }
+  a.q = static_cast<const char*>(q), a.q_out = static_cast<char*>(q_out);
+  a.q_stride = q_stride * elem_bytes(type), a.q_out_stride = q_out_stride * elem_bytes(q_out_type);
+  a.freq = freq, a.q_heads = n_q_heads, a.rot = rot_dim, a.interleaved = interleaved != 0, a.q_out_type = q_out_type;
+  if (a.c.b.n_tokens == 0) return QTEA_OK;
+  const int heads = 64 / (cache->head_dim / 8);
+  a.tasks = (n_q_heads + heads - 1) / heads + 2 * ((cache->n_heads + heads - 1) / heads);
+  a.per_part = a.tasks, a.parts = 1;
+  const int64_t blocks = std::min<int64_t>((int64_t(a.c.b.n_tokens) * a.parts + kThreads / 64 - 1) / (kThreads / 64), 1 << 20);
+  for_kernel(cache->format, type, [&](auto fmt, auto ty) {
+    hipLaunchKernelGGL((kv_append_rotated_kernel<decltype(fmt)::value, decltype(ty)::value>), dim3(uint32_t(blocks)), dim3(kThreads), 0,
+                       static_cast<hipStream_t>(stream), a);
   });
   return hipGetLastError() == hipSuccess ? QTEA_OK : QTEA_ERR_HIP;
 }

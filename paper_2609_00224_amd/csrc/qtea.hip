@@ -400,7 +400,7 @@ const char* qtea_status_string(int status) {
     case QTEA_ERR_INVALID_ARG: return "invalid argument";
     case QTEA_ERR_BAD_TRIT: return "trit outside {-1, 0, +1}";
     case QTEA_ERR_BAD_RESIDUAL: return "bad residual position or salient column list";
-    case QTEA_ERR_BATCH: return "batch outside [1, 16]";
+    case QTEA_ERR_BATCH: return "batch outside [1, 16] (4-bit weights: [1, 64])";
     case QTEA_ERR_WORKSPACE: return "workspace or packed buffer too small";
     case QTEA_ERR_HIP: return "HIP runtime error";
     case QTEA_ERR_NOT_POSITIVE: return "Hessian not positive definite";

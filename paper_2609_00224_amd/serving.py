@@ -1,6 +1,7 @@
 """Serving operators of libqtea.so (include/qtea_serve.h): a paged key/value
-cache in 16, 8 or 4 bits, causal attention of a batch's newest tokens over
-it, and the verification of drafted tokens.
+cache in 16, 8 or 4 bits with the rotation of queries and keys by their
+positions, causal attention of a batch's newest tokens over it, and the
+verification of drafted tokens.
 
 As the rest of the binding, these functions marshal arguments only; every
 step runs in the kernels of ``csrc/kv_cache.hip``, ``csrc/paged_attn.hip`` and
@@ -133,6 +134,34 @@ def qtea_kv_append(cache: KvCache, k, v, q_start, kv_len, page_table, stream=Non
     (fp16, bf16 or fp32; a token's part contiguous, tokens any stride), at
     their sequences' ends (kv_len already counts them)."""
     _dense("qtea_kv_append", cache, k, v, q_start, kv_len, page_table, stream)
+
+
+def qtea_kv_append_rotated(cache: KvCache, Q, k, v, q_start, kv_len, page_table, freq, q_out, interleaved: bool = False, stream=None):
+    """qtea_kv_append with queries and keys turned by their positions on the
+    way: Q [tokens][n_q_heads][head_dim] (of k's type) goes to q_out (the same
+    shape, fp16, bf16 or fp32; Q itself for in place), k to the cache, v as it
+    is.  freq: fp32 [rot_dim / 2], the angle of a pair per position; pairs are
+    channels i and i + rot_dim / 2, or interleaved 2i and 2i + 1; channels from
+    rot_dim on are not turned.  Q and q_out may be None: keys and values only."""
+    ks, vs = _rows(cache, k, cache.n_heads, "k"), _rows(cache, v, cache.n_heads, "v")
+    n = k.shape[0]
+    if k.dtype != v.dtype or v.shape[0] != n:
+        raise ValueError("k and v: one type, one number of tokens")
+    if freq.dtype is not _F32 or not freq.is_contiguous() or freq.get_device() != cache.device_index:
+        raise ValueError("freq: contiguous fp32 of the cache's device")
+    heads = qs = os_ = kind = 0
+    if (Q is None) != (q_out is None):
+        raise ValueError("Q and q_out come together")
+    if Q is not None:
+        heads = Q.shape[1] if Q.dim() == 3 else 0
+        qs, os_, kind = _rows(cache, Q, heads, "Q"), _rows(cache, q_out, heads, "q_out"), _type(q_out, "q_out")
+        if Q.dtype != k.dtype or Q.shape[0] != n or q_out.shape[0] != n or heads == 0:
+            raise ValueError("Q, k and v: one type; Q, q_out, k and v: one number of tokens")
+    b = _batch(cache, n, q_start, kv_len, page_table)
+    if n == 0:
+        return
+    _call("qtea_kv_append_rotated", cache.device_index, stream, cache.desc, b, None if Q is None else Q.data_ptr(), k.data_ptr(), v.data_ptr(),
+          _type(k, "k and v"), qs, ks, vs, heads, freq.data_ptr(), 2 * freq.numel(), bool(interleaved), None if Q is None else q_out.data_ptr(), kind, os_)
 
 
 def qtea_kv_read(cache: KvCache, q_start, kv_len, page_table, k, v, stream=None):
