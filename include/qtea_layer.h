@@ -91,7 +91,7 @@ int qtea_silu_mul(const void* gate, const void* up, int type, int64_t gate_strid
  * qtea_kv_append's rule for E2M1: 4.25 bits per weight.  Every value of such a
  * block is an fp16 (and a bf16) value, and packing such values again gives
  * the same ones.  A block with a NaN or an infinity is NaN.
- * The packed buffer is opaque; N is 1 .. 2^31 - 1, K 1 .. 2^30.
+ * The packed buffer is opaque; N is 1 .. 2^31 - 1, K 1 .. 2^24.
  */
 int qtea_w4_packed_bytes(int64_t N, int64_t K, int64_t* out_bytes);
 

@@ -3,8 +3,11 @@
 // W [N][K] is packed in tiles of 16 rows by 128 columns, the left operand of four
 // matrix instructions: lane (q, r) = 16 q + r of a wave holds row r, columns
 // 32 q .. 32 q + 31, a block, as 16 bytes (code j in half j % 2 of byte j / 2).
-//   codes   [ceil(N/16)][ceil(K/128)][64 lanes][16 bytes]
-//   scales  [ceil(N/16)][ceil(K/512)][64 lanes][4 bytes], byte i that of tile 4 u + i
+//   codes   [ceil(K/128)][ceil(N/16)][64 lanes][16 bytes]
+//   scales  [ceil(K/512)][ceil(N/16)][64 lanes][4 bytes], byte i that of tile 4 u + i
+// Strips of 16 rows lie next to each other, so that what the waves of the chip
+// read at a time, a column of tiles, is one piece (against strip after strip:
+// 128257 x 4096 at 16 rows 50.0 us for 55.6, at one 49.4 for 53.0).
 // Rows and columns past the matrix are zeros.
 #include <algorithm>
 #include <type_traits>
@@ -14,7 +17,7 @@
 namespace qtea_serve {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;
 constexpr int kTile = 1024;       // bytes of a tile's codes
 constexpr int kUnitScales = 256;  // bytes of four tiles' scales
 
@@ -22,7 +25,7 @@ struct Layout {
   int64_t strips, tiles, units, scales_at, bytes;  // of 16 rows; tiles and units of four tiles of a strip
 };
 bool make_layout(int64_t N, int64_t K, Layout* l) {
-  if (N < 1 || K < 1 || N > INT32_MAX || K > (int64_t(1) << 30)) return false;
+  if (N < 1 || K < 1 || N > INT32_MAX || K > (1 << 24)) return false;
   l->strips = (N + 15) / 16, l->tiles = (K + 127) / 128, l->units = (l->tiles + 3) / 4;
   l->scales_at = l->strips * l->tiles * kTile;
   l->bytes = l->scales_at + l->strips * l->units * kUnitScales;
@@ -34,7 +37,7 @@ struct PackArgs {
   uint8_t* codes;
   uint8_t* scales;
   int64_t stride;  // bytes
-  int64_t tiles, units, total;  // total: strips * units * 256 blocks
+  int64_t strips, tiles, units, total;  // total: strips * units * 256 blocks
   int32_t N, K;
   bool wide;
 };
@@ -70,9 +73,9 @@ __global__ __launch_bounds__(kThreads) void w4_pack_kernel(const PackArgs a) {
       u32x4 v;
 #pragma unroll
       for (int j = 0; j < 4; ++j) v[j] = block_codes<QTEA_KV_E2M1>(x[j], e)[0];
-      *reinterpret_cast<u32x4*>(a.codes + (k.strip * a.tiles + k.tile) * kTile + k.lane * 16) = v;
+      *reinterpret_cast<u32x4*>(a.codes + (k.tile * a.strips + k.strip) * kTile + k.lane * 16) = v;
     }
-    a.scales[(k.strip * a.units + (k.tile >> 2)) * kUnitScales + k.lane * 4 + (k.tile & 3)] = uint8_t(e);
+    a.scales[((k.tile >> 2) * a.strips + k.strip) * kUnitScales + k.lane * 4 + (k.tile & 3)] = uint8_t(e);
   }
 }
 
@@ -82,8 +85,8 @@ __global__ __launch_bounds__(kThreads) void w4_unpack_kernel(const PackArgs a) {
     const Block k = block_of(a, b);
     const int64_t row = k.strip * 16 + (k.lane & 15), col = k.tile * 128 + (k.lane >> 4) * 32;
     if (k.tile >= a.tiles || row >= a.N) continue;
-    const float s = scale_value(a.scales[(k.strip * a.units + (k.tile >> 2)) * kUnitScales + k.lane * 4 + (k.tile & 3)]);
-    const u32x4 v = *reinterpret_cast<const u32x4*>(a.codes + (k.strip * a.tiles + k.tile) * kTile + k.lane * 16);
+    const float s = scale_value(a.scales[((k.tile >> 2) * a.strips + k.strip) * kUnitScales + k.lane * 4 + (k.tile & 3)]);
+    const u32x4 v = *reinterpret_cast<const u32x4*>(a.codes + (k.tile * a.strips + k.strip) * kTile + k.lane * 16);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const f32x2 y[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v[j], 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v[j], 1.0f, 1),
@@ -105,8 +108,10 @@ struct GemmArgs {
   const uint8_t* x_scale;
   char* y;
   int64_t x_stride, x_scale_stride, y_stride;  // bytes
-  int32_t N, K, tiles, units, batch, y_type;
-  bool x_wide;
+  int32_t x_bytes, x_scale_bytes;              // of X and its scales, first row to last
+  int32_t N, K, strips, tiles, units, batch, y_type;
+  bool x_dwords, y_wide;      // rows of X are 4-byte aligned, of Y (16 bits) 8-byte
+  int32_t parts;              // waves that share a strip's units
 };
 
 // The 16-bit type whose matrix instructions a product runs on.  E4M3 activations
@@ -115,95 +120,335 @@ struct GemmArgs {
 template <int XT>
 using Type = std::conditional_t<XT == QTEA_F16, F16, BF16>;
 
-// A lane's 32 activations of a tile as the matrix instructions' right operand.
-struct Acts {
-  u32x4 v[4];
-};
+// 8 columns of the lane's block as the left operand: exact in either type.
+template <class T>
+__device__ __forceinline__ u32x4 weights(uint32_t w, float s) {
+  return u32x4{T::template e2m1<0>(w, s), T::template e2m1<1>(w, s), T::template e2m1<2>(w, s), T::template e2m1<3>(w, s)};
+}
 
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+
+// A lane's four rows n0.. of one result column (a row of Y).
+__device__ __forceinline__ void store_y(const GemmArgs& a, int b, int64_t n0, f32x4 c) {
+  if (b >= a.batch || n0 >= a.N) return;
+  char* row = a.y + b * a.y_stride;
+  const int size = a.y_type == QTEA_F32 ? 4 : 2;
+  if (a.y_type == QTEA_F32 && n0 + 4 <= a.N) {
+    *reinterpret_cast<f32x4u*>(row + 4 * n0) = c;
+    return;
+  }
+  const u32x2 v = a.y_type == QTEA_F16 ? u32x2{F16::pack(c[0], c[1]), F16::pack(c[2], c[3])} : u32x2{BF16::pack(c[0], c[1]), BF16::pack(c[2], c[3])};
+  if (a.y_wide && n0 + 4 <= a.N) {
+    *reinterpret_cast<u32x2*>(row + 2 * n0) = v;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (n0 + i >= a.N) break;
+    if (size == 4) *reinterpret_cast<float*>(row + 4 * (n0 + i)) = c[i];
+    else *reinterpret_cast<uint16_t*>(row + 2 * (n0 + i)) = uint16_t(v[i / 2] >> (16 * (i & 1)));
+  }
+}
+
+// A strip's tile and scales from an address that is the same for the wave, which
+// the compiler is to keep in scalar registers (and add the lanes' parts in the
+// load, where it would carry 64-bit addresses a lane).
+template <class V>
+using global_t = __attribute__((address_space(1))) const V;
+__device__ __forceinline__ uint64_t scalar(const uint8_t* p) {
+  uint64_t at = reinterpret_cast<uint64_t>(p);
+  asm volatile("" : "+s"(at));
+  return at;
+}
+__device__ __forceinline__ u32x4 load_codes(uint64_t p, uint32_t lane, int r) { return *reinterpret_cast<global_t<u32x4>*>(p + lane * 16 + r * kTile); }
+__device__ __forceinline__ uint32_t load_scale4(uint64_t p, uint32_t lane, int r) { return *reinterpret_cast<global_t<uint32_t>*>(p + lane * 4 + r * kUnitScales); }
+
+// A value that is computed where it is used instead of being held in
+// registers across the loop.
+__device__ __forceinline__ int fresh(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// X and its scales by way of descriptors: offsets past the end give zeros
+// without a fetch, and 16-byte loads are aligned to 4 bytes.
+struct XBuf {
+  __amdgpu_buffer_rsrc_t x, scale;
+};
 template <int XT>
-__device__ __forceinline__ Acts load_acts(const GemmArgs& a, const char* row, const uint8_t* srow, int tile, int q) {
-  Acts r;
-  const int k0 = tile * 128 + 32 * q;
+__device__ __forceinline__ XBuf x_buffers(const GemmArgs& a) {
+  XBuf b;
+  b.x = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(a.x), 0, a.x_bytes, 0x00020000);
+  if constexpr (XT == QTEA_E4M3) b.scale = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.x_scale), 0, a.x_scale_bytes, 0x00020000);
+  return b;
+}
+
+// 8 activations k.. of a row: 16-bit values, or codes and their block's scale.
+// Zeros past K.
+template <int XT>
+struct Piece {
+  std::conditional_t<XT == QTEA_E4M3, u32x2, u32x4> v;
+  uint32_t scale;
+};
+constexpr uint32_t kPastEnd = 0x80000000u;  // an offset past every descriptor's end
+// (Every lane of a wave takes part, whatever it needs: a number of loads that does
+// not depend on the call lets the wave wait for the one it needs.)  ODD: rows
+// that are 2-byte aligned.
+template <int XT, bool ODD>
+__device__ __forceinline__ Piece<XT> load_piece(const GemmArgs& a, const XBuf& xb, int row, int k) {
+  Piece<XT> r;
+  const bool in = k < a.K && row < a.batch;
+  const uint32_t at = in ? uint32_t(k) * elem_bytes(XT) : kPastEnd, row_at = uint32_t(row) * uint32_t(a.x_stride);
   if constexpr (XT == QTEA_E4M3) {  // (K is a multiple of 32)
-    const bool in = k0 < a.K;
-    const float s = scale_of(in ? srow[k0 / 32] : 127u);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const u32x4 zero = {0, 0, 0, 0};
-      const u32x4 c = in ? *reinterpret_cast<const u32x4*>(row + k0 + 16 * i) : zero;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        r.v[2 * i + j / 2][j % 2 * 2] = BF16::e4m3<false>(c[j], s);
-        r.v[2 * i + j / 2][j % 2 * 2 + 1] = BF16::e4m3<true>(c[j], s);
-      }
-    }
+    r.v = __builtin_amdgcn_raw_buffer_load_b64(xb.x, at, row_at, 0);
+    r.scale = uint8_t(__builtin_amdgcn_raw_buffer_load_b8(xb.scale, in ? uint32_t(k) / 32 : kPastEnd, uint32_t(row) * uint32_t(a.x_scale_stride), 0));
+  } else if constexpr (!ODD) {
+    r.v = __builtin_amdgcn_raw_buffer_load_b128(xb.x, at, row_at, 0);
   } else {
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      const int k = k0 + 8 * m, n = a.K - k;
-      if (a.x_wide && n >= 8) {
-        r.v[m] = *reinterpret_cast<const u32x4*>(row + 2 * int64_t(k));
-      } else {
-        const uint16_t* p = reinterpret_cast<const uint16_t*>(row) + k;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t lo = 2 * i < n ? p[2 * i] : 0u, hi = 2 * i + 1 < n ? p[2 * i + 1] : 0u;
-          r.v[m][i] = lo | hi << 16;
-        }
-      }
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t lo = uint16_t(__builtin_amdgcn_raw_buffer_load_b16(xb.x, at + 4 * i, row_at, 0)), hi = uint16_t(__builtin_amdgcn_raw_buffer_load_b16(xb.x, at + 4 * i + 2, row_at, 0));
+      r.v[i] = lo | hi << 16;
     }
   }
   return r;
 }
-
-// 16 rows of W times 16 of X over 128 columns; `scale`: the lane's block's.  The
-// weights are exact in either type.
-template <class T>
-__device__ __forceinline__ f32x4 tile_product(u32x4 w, uint32_t scale, const Acts& x, f32x4 c) {
-  const float s = scale_of(scale);
-#pragma unroll
-  for (int m = 0; m < 4; ++m) {
-    const u32x4 A = {T::template e2m1<0>(w[m], s), T::template e2m1<1>(w[m], s), T::template e2m1<2>(w[m], s), T::template e2m1<3>(w[m], s)};
-    c = T::mfma16(A, x.v[m], c);
-  }
-  return c;
-}
-
-__device__ __forceinline__ void store_y(const GemmArgs& a, int b, int64_t n0, f32x4 c) {
-  if (b >= a.batch) return;
-  char* row = a.y + b * a.y_stride;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (n0 + i >= a.N) break;
-    if (a.y_type == QTEA_F32) store1<QTEA_F32>(row + 4 * (n0 + i), c[i]);
-    else if (a.y_type == QTEA_F16) store1<QTEA_F16>(row + 2 * (n0 + i), c[i]);
-    else store1<QTEA_BF16>(row + 2 * (n0 + i), c[i]);
-  }
-}
-
-// A workgroup takes 16 rows of W and 16 of X, its waves the tiles in turn.
+// As 16-bit values.
 template <int XT>
-__global__ __launch_bounds__(kThreads) void w4_gemm_kernel(const GemmArgs a) {
-  __shared__ f32x4 s_sum[kThreads / 64][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane >> 4;
-  const int64_t strip = blockIdx.x;
-  const int b = blockIdx.y * 16 + (lane & 15), bx = min(b, a.batch - 1);
-  const char* xrow = a.x + bx * a.x_stride;
-  const uint8_t* srow = XT == QTEA_E4M3 ? a.x_scale + bx * a.x_scale_stride : nullptr;
-  const uint8_t* codes = a.codes + strip * a.tiles * kTile + lane * 16;
-  const uint8_t* scales = a.scales + strip * a.units * kUnitScales + lane * 4;
-  f32x4 c = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int t = wave; t < a.tiles; t += kThreads / 64) {
-    const u32x4 w = *reinterpret_cast<const u32x4*>(codes + int64_t(t) * kTile);
-    const uint32_t s = scales[int64_t(t >> 2) * kUnitScales + (t & 3)];
-    c = tile_product<Type<XT>>(w, s, load_acts<XT>(a, xrow, srow, t, q), c);
-  }
-  s_sum[wave][lane] = c;
-  __syncthreads();
-  if (wave != 0) return;
+__device__ __forceinline__ u32x4 piece_value(const GemmArgs& a, const Piece<XT>& p, int k) {
+  if constexpr (XT == QTEA_E4M3) {
+    const float s = scale_of(p.scale);
+    return u32x4{BF16::e4m3<false>(p.v[0], s), BF16::e4m3<true>(p.v[0], s), BF16::e4m3<false>(p.v[1], s), BF16::e4m3<true>(p.v[1], s)};
+  } else {
+    u32x4 v = p.v;
+    if (k + 8 > a.K) {  // a row's last values: what follows them is not its own
+      const int n = a.K - k;
 #pragma unroll
-  for (int i = 1; i < kThreads / 64; ++i) c += s_sum[i][lane];
-  store_y(a, b, strip * 16 + 4 * q, c);
+      for (int i = 0; i < 4; ++i) v[i] = 2 * i + 1 < n ? v[i] : (2 * i < n ? v[i] & 0xffffu : 0u);
+    }
+    return v;
+  }
+}
+
+// LDS holds a unit's right operands as the lanes take them: 16-byte pieces
+// [tile][CT][instruction][64 lanes], the lane within them turned by (tile, instruction)
+// so that the writes, 64 consecutive pieces of a row, meet different banks.
+template <int CT>
+__device__ __forceinline__ uint32_t piece_at(int tile, int ct, int m, int lane) {
+  return uint32_t(((tile * CT + ct) * 4 + m) * 64 + (lane ^ (m + 4 * tile)));
+}
+// Where the piece of `lane` in a row's 64 goes.
+template <int CT>
+__device__ __forceinline__ uint32_t piece_to(int row, int lane) {
+  return piece_at<CT>(lane / 16, row / 16, lane & 3, (lane / 4 & 3) * 16 + (row & 15));
+}
+
+// Few strips: the waves of a workgroup share R strips' units, each with its own
+// 16 rows of X, by way of LDS of its own (no barriers; a row's 64 pieces come in one
+// coalesced load, where the lanes' own pieces would touch 64 lines an instruction).
+// While a unit is multiplied, the next one is on its way.
+template <int XT, int R, int ROWS, bool ODD>
+__global__ __launch_bounds__(kThreads) void w4_gemm_split_kernel(const GemmArgs a) {
+  using T = Type<XT>;
+  extern __shared__ u32x4 s_x[];  // [waves][4 tiles * 4 * 64]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), q = lane >> 4;
+  const int part = wave % a.parts;
+  const int64_t group = int64_t(blockIdx.x) * (kThreads / 64 / a.parts) + wave / a.parts;
+  const int64_t strip0 = min(group * R, int64_t(a.strips) - R);  // (the last groups: strips of others, again)
+  const int row0 = blockIdx.y * 16;
+  const XBuf xb = x_buffers<XT>(a);
+  u32x4* mine = s_x + wave * (4 * 4 * 64);
+  const int u0 = int(int64_t(a.units) * part / a.parts), u1 = int(int64_t(a.units) * (part + 1) / a.parts);
+  f32x4 c[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) c[r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  if (u0 < u1) {
+    const uint8_t* codes = a.codes + strip0 * kTile;
+    const uint8_t* scales = a.scales + strip0 * kUnitScales;
+    u32x4 w[4][R];
+    uint32_t sc[R], next[R];
+    Piece<XT> x[ROWS];
+    // tile j of unit u (past the last tile: that one again, times zeros)
+    auto load = [&](int u, int j) {
+      const uint64_t p = scalar(codes + int64_t(min(4 * u + j, a.tiles - 1)) * a.strips * kTile);
+#pragma unroll
+      for (int r = 0; r < R; ++r) w[j][r] = load_codes(p, lane, r);
+    };
+    auto load_scales = [&](int u, uint32_t (&to)[R]) {
+      const uint64_t p = scalar(scales + int64_t(u) * a.strips * kUnitScales);
+#pragma unroll
+      for (int r = 0; r < R; ++r) to[r] = load_scale4(p, lane, r);
+    };
+    auto load_x = [&](int u) {
+#pragma unroll
+      for (int i = 0; i < ROWS; ++i) x[i] = load_piece<XT, ODD>(a, xb, row0 + i, u * 512 + lane * 8);
+    };
+    auto write_x = [&](int u) {
+      const int at = fresh(lane);
+#pragma unroll
+      for (int i = 0; i < ROWS; ++i) mine[piece_to<1>(i, at)] = piece_value<XT>(a, x[i], u * 512 + lane * 8);
+    };
+    auto multiply = [&](int j) {
+      const int at = fresh(lane);
+      u32x4 B[4];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) B[m] = mine[piece_at<1>(j, 0, m, at)];
+      float f[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) f[r] = scale_of(sc[r] >> (8 * j) & 255u);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int r = 0; r < R; ++r) c[r] = T::mfma16(weights<T>(w[j][r][m], f[r]), B[m], c[r]);
+    };
+    load_x(u0);
+    load_scales(u0, sc);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      load(u0, j);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    write_x(u0);
+    for (int u = u0; u + 1 < u1; ++u) {
+      load_x(u + 1);
+      load_scales(u + 1, next);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        multiply(j);
+        __builtin_amdgcn_sched_barrier(0);
+        load(u + 1, j);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      write_x(u + 1);
+#pragma unroll
+      for (int r = 0; r < R; ++r) sc[r] = next[r];
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) multiply(j);
+  }
+  const int b = row0 + (lane & 15);
+  if (a.parts > 1) {
+    // the parts' sums, in order
+    f32x4* sums = reinterpret_cast<f32x4*>(s_x);  // [waves][R][64], in the waves' own places
+    f32x4* own = reinterpret_cast<f32x4*>(mine);
+#pragma unroll
+    for (int r = 0; r < R; ++r) own[r * 64 + lane] = c[r];
+    __syncthreads();
+    for (int r = part; r < R; r += a.parts) {
+      const f32x4* p = sums + (wave - part) * (4 * 4 * 64) + r * 64 + lane;
+      f32x4 sum = p[0];
+      for (int i = 1; i < a.parts; ++i) sum += p[i * (4 * 4 * 64)];
+      store_y(a, b, (strip0 + r) * 16 + 4 * q, sum);
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < R; ++r) store_y(a, b, (strip0 + r) * 16 + 4 * q, c[r]);
+  }
+}
+
+// Many strips: a workgroup's waves take R strips each over all columns, and share
+// the activations in LDS, a unit (512 columns) at a time, two units there: the
+// next one is loaded while this one is multiplied, one barrier a unit.
+template <int XT, int R, int CT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void w4_gemm_wide_kernel(const GemmArgs a) {
+  using T = Type<XT>;
+  constexpr int AHEAD = R == 4 ? 1 : 2;        // units of codes on the way
+  constexpr int ROWS = CT * 16 / WAVES;        // rows of X a wave brings
+  extern __shared__ u32x4 s_x[];  // [2][4 tiles * CT * 4 * 64]
+  constexpr int kBuf = 4 * CT * 4 * 64;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), q = lane >> 4;
+  const int64_t strip0 = min((int64_t(blockIdx.x) * WAVES + wave) * R, int64_t(a.strips) - R);  // (the last waves: strips of others, again)
+  const uint8_t* codes = a.codes + strip0 * kTile;
+  const uint8_t* scales = a.scales + strip0 * kUnitScales;
+  const XBuf xb = x_buffers<XT>(a);
+  u32x4 w[AHEAD][4][R];
+  uint32_t sc[AHEAD][R];
+  auto load = [&](int s, int u, int j) {
+    const uint64_t p = scalar(codes + int64_t(min(4 * u + j, a.tiles - 1)) * a.strips * kTile);  // (past the last tile: that one again, times zeros)
+#pragma unroll
+    for (int r = 0; r < R; ++r) w[s][j][r] = load_codes(p, lane, r);
+  };
+  auto load_scales = [&](int s, int u) {
+    const uint64_t p = scalar(scales + int64_t(min(u, a.units - 1)) * a.strips * kUnitScales);
+#pragma unroll
+    for (int r = 0; r < R; ++r) sc[s][r] = load_scale4(p, lane, r);
+  };
+  // A wave brings whole rows of a unit, 8 columns a lane.
+  Piece<XT> x[ROWS];
+  auto load_x = [&](int u) {
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) x[i] = load_piece<XT, false>(a, xb, i * WAVES + wave, u * 512 + lane * 8);
+  };
+  auto write_x = [&](int u) {
+    const int at = fresh(lane);
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) s_x[(u & 1) * kBuf + piece_to<CT>(i * WAVES + wave, at)] = piece_value<XT>(a, x[i], u * 512 + lane * 8);
+  };
+  f32x4 c[CT][R];
+#pragma unroll
+  for (int t = 0; t < CT; ++t)
+#pragma unroll
+    for (int r = 0; r < R; ++r) c[t][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+  load_x(0);
+#pragma unroll
+  for (int s = 0; s < AHEAD; ++s) {
+    load_scales(s, s);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      load(s, s, j);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  write_x(0);
+  __syncthreads();
+  for (int u0 = 0; u0 < a.units; u0 += AHEAD) {
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s) {
+      const int u = u0 + s;
+      if (u >= a.units) break;
+      load_x(u + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      const u32x4* buf = s_x + (u & 1) * kBuf;
+      u32x4 B[2][CT];
+      auto read_x = [&](int step) {
+        const int at = fresh(lane);
+#pragma unroll
+        for (int t = 0; t < CT; ++t) B[step & 1][t] = buf[piece_at<CT>(step / 4, t, step & 3, at)];
+      };
+      read_x(0);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float f[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) f[r] = scale_of(sc[s][r] >> (8 * j) & 255u);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          if (j < 3 || m < 3) read_x(4 * j + m + 1);  // the next instructions' right operands, a step ahead
+          __builtin_amdgcn_sched_barrier(0);
+          u32x4 A[R];
+#pragma unroll
+          for (int r = 0; r < R; ++r) A[r] = weights<T>(w[s][j][r][m], f[r]);
+#pragma unroll
+          for (int t = 0; t < CT; ++t)
+#pragma unroll
+            for (int r = 0; r < R; ++r) c[t][r] = T::mfma16(A[r], B[m & 1][t], c[t][r]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        load(s, u + AHEAD, j);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      load_scales(s, u + AHEAD);
+      if (u + 1 < a.units) write_x(u + 1);
+      __syncthreads();
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < CT; ++t)
+#pragma unroll
+    for (int r = 0; r < R; ++r) store_y(a, t * 16 + (lane & 15), (strip0 + r) * 16 + 4 * q, c[t][r]);
 }
 
 }  // namespace
@@ -218,7 +463,7 @@ bool pack_args(const void* packed, int64_t N, int64_t K, const void* W, int type
   if (!stride_ok(w_stride, K) || !aligned_to_elem(W, type)) return false;
   a->w = static_cast<char*>(const_cast<void*>(W));
   a->codes = static_cast<uint8_t*>(const_cast<void*>(packed)), a->scales = a->codes + l->scales_at;
-  a->stride = w_stride * elem_bytes(type), a->tiles = l->tiles, a->units = l->units, a->total = l->strips * l->units * 256;
+  a->stride = w_stride * elem_bytes(type), a->strips = l->strips, a->tiles = l->tiles, a->units = l->units, a->total = l->strips * l->units * 256;
   a->N = int32_t(N), a->K = int32_t(K), a->wide = rows_aligned16(W, w_stride, type);
   return true;
 }
@@ -231,6 +476,91 @@ void for_type(int type, Launch launch) {
 }
 
 dim3 pack_blocks(int64_t total) { return dim3(uint32_t(std::min<int64_t>((total + kThreads - 1) / kThreads, 1 << 20))); }
+
+int compute_units() {
+  static std::atomic<int> known[qtea_detail::kMaxDevices];
+  return qtea_detail::per_current_device(known, [](int dev) {
+    int n = 0;
+    return hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess ? n : 0;
+  });
+}
+
+using std::integral_constant;
+
+template <int XT, int R, int CT, int WAVES>
+int run_wide(const GemmArgs& a, hipStream_t st) {
+  const auto kernel = w4_gemm_wide_kernel<XT, R, CT, WAVES>;
+  static std::atomic<int> allowed[qtea_detail::kMaxDevices];
+  constexpr int lds = 2 * 4 * CT * 4 * 64 * 16;
+  if (qtea_detail::allow_lds(reinterpret_cast<const void*>(kernel), lds, allowed) != hipSuccess) return QTEA_ERR_HIP;
+  const int64_t blocks = (int64_t(a.strips) + R * WAVES - 1) / (R * WAVES);
+  hipLaunchKernelGGL(kernel, dim3(uint32_t(blocks)), dim3(64 * WAVES), lds, st, a);
+  return hipGetLastError() == hipSuccess ? QTEA_OK : QTEA_ERR_HIP;
+}
+
+template <int XT, int R, int ROWS, bool ODD>
+int run_split(const GemmArgs& a, hipStream_t st) {
+  const auto kernel = w4_gemm_split_kernel<XT, R, ROWS, ODD>;
+  static std::atomic<int> allowed[qtea_detail::kMaxDevices];
+  constexpr int lds = kThreads / 64 * 4 * 4 * 64 * 16;
+  if (qtea_detail::allow_lds(reinterpret_cast<const void*>(kernel), lds, allowed) != hipSuccess) return QTEA_ERR_HIP;
+  const int64_t groups = (int64_t(a.strips) + R - 1) / R;
+  const int per = kThreads / 64 / a.parts;
+  hipLaunchKernelGGL(kernel, dim3(uint32_t((groups + per - 1) / per), uint32_t((a.batch + 15) / 16)), dim3(kThreads), lds, st, a);
+  return hipGetLastError() == hipSuccess ? QTEA_OK : QTEA_ERR_HIP;
+}
+
+// Which kernel, by strips a CU.  With five or more a wave can have whole strips
+// to itself (28672 x 4096 at 16 rows of E4M3: 13.3 us, 16.0 with its columns split;
+// 14336 x 4096: 11.1 and 8.8); past 16 rows with three or more, since the other
+// kernel reads the weights again for each 16 (16384 x 4096 at 40 rows 18.6 us
+// and 21.3).
+template <int XT>
+int run_gemm(GemmArgs a, int cus, hipStream_t st) {
+  const int ct = (a.batch + 15) / 16;
+  if (a.x_dwords && a.strips >= (ct == 1 ? 5 : 3) * cus) {
+    // Strips and waves of a workgroup: the fewest strips on the CU that has most,
+    // then the most a workgroup (a wave's operands from LDS serve all its strips:
+    // 128257 x 4096 at 64 rows 71 us with four, 86 with two, 110 with one).  Past 32
+    // rows one workgroup fills a CU's LDS and has eight waves.
+    int R = 1, waves = 8;
+    int64_t least = INT64_MAX;
+    for (int r = 1; r <= 4; r *= 2)
+      for (int w = 8; w >= (r == 4 || ct > 2 ? 8 : 4); w -= 4) {
+        const int64_t blocks = (int64_t(a.strips) + r * w - 1) / (r * w), most = (blocks + cus - 1) / cus * r * w;
+        if (most < least || (most == least && r * w > R * waves)) least = most, R = r, waves = w;
+      }
+    const auto with = [&](auto cols) {
+      constexpr int CT = decltype(cols)::value;
+      if (R == 4) return run_wide<XT, 4, CT, 8>(a, st);
+      if (waves == 8) return R == 2 ? run_wide<XT, 2, CT, 8>(a, st) : run_wide<XT, 1, CT, 8>(a, st);
+      if constexpr (CT <= 2) return R == 2 ? run_wide<XT, 2, CT, 4>(a, st) : run_wide<XT, 1, CT, 4>(a, st);
+      return int(QTEA_ERR_HIP);  // (not reached)
+    };
+    if (ct == 1) return with(integral_constant<int, 1>());
+    if (ct == 2) return with(integral_constant<int, 2>());
+    return ct == 3 ? with(integral_constant<int, 3>()) : with(integral_constant<int, 4>());
+  }
+  // Strips a group: the most that leave groups for six CUs of ten (10240 x 8192 at 16
+  // rows 12.5 us with four, 16.2 with two; 8192 x 28672: 37.5 with four, that is
+  // half of the CUs, 30.5 with two); waves a group: eight a CU, if there are units.
+  int R = a.x_dwords ? 4 : 2;
+  while (R > 1 && (a.strips < R || int64_t(a.strips) * ct * 10 < int64_t(R) * 6 * cus)) R /= 2;
+  a.parts = 1;
+  while (a.parts < kThreads / 64 && a.parts < a.units && (int64_t(a.strips) + R - 1) / R * a.parts < 8 * int64_t(cus)) a.parts *= 2;
+  const auto with = [&](auto strips) {
+    constexpr int RR = decltype(strips)::value;
+    if constexpr (XT != QTEA_E4M3 && RR < 4) {
+      if (!a.x_dwords) return run_split<XT, RR, 16, true>(a, st);
+    }
+    if (a.batch == 1) return run_split<XT, RR, 1, false>(a, st);
+    if (a.batch <= 4) return run_split<XT, RR, 4, false>(a, st);
+    if (a.batch <= 8) return run_split<XT, RR, 8, false>(a, st);
+    return run_split<XT, RR, 16, false>(a, st);
+  };
+  if (R == 4) return with(integral_constant<int, 4>());
+  return R == 2 ? with(integral_constant<int, 2>()) : with(integral_constant<int, 1>());
+}
 
 }  // namespace
 
@@ -284,14 +614,21 @@ int qtea_w4_gemm_lowbatch(const void* packed, int64_t packed_bytes, int64_t N, i
   a.codes = static_cast<const uint8_t*>(packed), a.scales = a.codes + l.scales_at;
   a.x = static_cast<const char*>(X), a.x_scale = x_scale, a.y = static_cast<char*>(Y);
   a.x_stride = x_stride * elem_bytes(x_type), a.x_scale_stride = x_scale_stride, a.y_stride = y_stride * elem_bytes(y_type);
-  a.N = int32_t(N), a.K = int32_t(K), a.tiles = int32_t(l.tiles), a.units = int32_t(l.units), a.batch = batch, a.y_type = y_type;
-  a.x_wide = rows_aligned16(X, x_stride, x_type);
-  const dim3 grid(uint32_t(l.strips), uint32_t((batch + 15) / 16));
+  a.N = int32_t(N), a.K = int32_t(K), a.strips = int32_t(l.strips), a.tiles = int32_t(l.tiles), a.units = int32_t(l.units);
+  a.batch = batch, a.y_type = y_type;
+  const int64_t x_bytes = (batch - 1) * a.x_stride + K * elem_bytes(x_type), sc_bytes = x_scale ? (batch - 1) * x_scale_stride + K / 32 : 0;
+  if (x_bytes > (1 << 30) || sc_bytes > (1 << 30)) return QTEA_ERR_INVALID_ARG;
+  // (a last dword may be half X's: the other half is read and not used)
+  a.x_bytes = int32_t((x_bytes + 3) & ~int64_t(3)), a.x_scale_bytes = int32_t(sc_bytes);
+  a.x_dwords = x_type == QTEA_E4M3 || ((reinterpret_cast<uintptr_t>(X) | (batch > 1 ? uint64_t(a.x_stride) : 0)) % 4 == 0);
+  if (!a.x_dwords) a.x_bytes = int32_t(x_bytes);
+  a.y_wide = (reinterpret_cast<uintptr_t>(Y) | uint64_t(a.y_stride)) % 8 == 0;
+  const int cus = compute_units();
+  if (cus == 0) return QTEA_ERR_HIP;
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  if (x_type == QTEA_F16) hipLaunchKernelGGL((w4_gemm_kernel<QTEA_F16>), grid, dim3(kThreads), 0, st, a);
-  else if (x_type == QTEA_BF16) hipLaunchKernelGGL((w4_gemm_kernel<QTEA_BF16>), grid, dim3(kThreads), 0, st, a);
-  else hipLaunchKernelGGL((w4_gemm_kernel<QTEA_E4M3>), grid, dim3(kThreads), 0, st, a);
-  return hipGetLastError() == hipSuccess ? QTEA_OK : QTEA_ERR_HIP;
+  if (x_type == QTEA_F16) return run_gemm<QTEA_F16>(a, cus, st);
+  if (x_type == QTEA_BF16) return run_gemm<QTEA_BF16>(a, cus, st);
+  return run_gemm<QTEA_E4M3>(a, cus, st);
 }
 
 }  // extern "C"

@@ -98,14 +98,38 @@ def test_whole_numbers_are_exact(N, K, batch, x):
     assert np.array_equal(Y.double().cpu().numpy(), v @ W.T)
 
 
+@pytest.mark.parametrize("x", ["f16", "bf16", "e4m3"])
+@pytest.mark.parametrize("batch", [1, 8, 16, 17, 32, 33, 48, 64])
+@pytest.mark.parametrize("N,K", [(12290, 96), (20481, 32), (20500, 544), (32000, 160), (61440, 1056), (131073, 64)])
+def test_many_rows_of_weights(N, K, batch, x):
+    """Five and more strips of 16 rows a CU (three past 16 rows of X): every
+    count of strips a wave takes, a unit of columns and more; exact sums."""
+    rng = np.random.default_rng([N, K, batch])
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(N + batch)
+    steps = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6, -0.5, -1, -1.5, -2, -3, -4, -6], device="cuda")
+    W = steps[torch.randint(0, 15, (N, K), generator=gen, device="cuda")]
+    v = rng.integers(-8, 9, (batch, K)).astype(np.float64)
+    X, xs = _dev(v, "f16" if x == "e4m3" else x), None
+    if x == "e4m3":
+        code, scale = sv.encode(v, "e4m3")
+        X, xs = torch.from_numpy(code).cuda(), torch.from_numpy(scale).cuda()
+    room = torch.full((batch + 1, N + 3), 7.0, device="cuda")
+    q.qtea_w4_gemm_lowbatch(q.pack_matrix_w4(W), X, room[:batch, :N], x_scale=xs)
+    want = torch.from_numpy(v).float().cuda() @ W.T  # whole halves below 2^24: exact in any order
+    assert torch.equal(room[:batch, :N], want)
+    assert (room[batch:] == 7).all() and (room[:, N:] == 7).all()
+
+
+@pytest.mark.parametrize("N", [90, 24000])
 @pytest.mark.parametrize("K,shift,pad", [(1000, 0, 8), (1000, 1, 0), (999, 0, 0), (1024, 3, 2), (4096, 0, 1), (130, 5, 6)])
-def test_rows_of_any_stride(K, shift, pad):
+def test_rows_of_any_stride(K, shift, pad, N):
     rng = np.random.default_rng([K, shift])
-    W = rng.choice([0, 0.5, 1, 3], (90, K))
+    W = rng.choice([0, 0.5, 1, 3], (N, K))
     v = rng.integers(-4, 5, (7, K)).astype(np.float64)
     wide = torch.full((7, shift + K + pad), float("nan"), dtype=torch.float16, device="cuda")
     wide[:, shift:shift + K] = _dev(v, "f16")
-    Y = torch.empty((7, 90), device="cuda")
+    Y = torch.empty((7, N), device="cuda")
     q.qtea_w4_gemm_lowbatch(q.pack_matrix_w4(_dev(W, "f16")), wide[:, shift:shift + K], Y)
     assert np.array_equal(Y.double().cpu().numpy(), v @ W.T)
 
