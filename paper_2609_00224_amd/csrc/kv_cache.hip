@@ -115,8 +115,9 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(const CacheArgs a) 
 // loaded a second time (it is in the L1).
 //
 // An angle is a product of a position (31 bits) and a frequency (24), in double with
-// what its rounding left, less the nearest multiple of pi / 2 in two doubles:
-// what is left is at most pi / 4 and exact to fp32's last bits.
+// what its rounding left, less the nearest multiple of pi / 2 in two doubles.  Of
+// what is left, at most pi / 4, the sine and cosine by their series, also in double (a
+// wave has one or two to find), and rounded once.
 struct RotateArgs {
   CacheArgs c;
   const char* q;
@@ -127,6 +128,7 @@ struct RotateArgs {
   int32_t tasks, parts, per_part;  // tasks of a token, waves that share them, tasks a wave
 };
 
+constexpr int64_t kFullWaves = 2048;
 constexpr int kMaxAngles = QTEA_KV_MAX_DIM / 2;
 
 __device__ __forceinline__ void turn_of(int pos, float freq, float& cs, float& sn) {
@@ -135,7 +137,11 @@ __device__ __forceinline__ void turn_of(int pos, float freq, float& cs, float& s
   // pi / 2 to 106 bits
   double r = __builtin_fma(n, -0x1.921fb54442d18p+0, angle);
   r = __builtin_fma(n, -0x1.1a62633145c07p-54, r) + rest;
-  const float x = float(r), s = sinf(x), c = cosf(x);
+  // r^13 / 13! and r^14 / 14! are below 2^-37 there
+  const double z = r * r;
+  const double ps = __builtin_fma(z, __builtin_fma(z, __builtin_fma(z, __builtin_fma(z, -1.0 / 39916800, 1.0 / 362880), -1.0 / 5040), 1.0 / 120), -1.0 / 6);
+  const double pc = __builtin_fma(z, __builtin_fma(z, __builtin_fma(z, __builtin_fma(z, __builtin_fma(z, 1.0 / 479001600, -1.0 / 3628800), 1.0 / 40320), -1.0 / 720), 1.0 / 24), -0.5);
+  const float s = float(__builtin_fma(r * z, ps, r)), c = float(__builtin_fma(z, pc, 1.0));
   const int quarter = int(int64_t(n) & 3);
   sn = quarter & 1 ? c : s;
   cs = quarter & 1 ? s : c;
@@ -175,50 +181,63 @@ __global__ __launch_bounds__(kThreads) void kv_append_rotated_kernel(const Rotat
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int at = base + (a.interleaved ? i / 2 : i);
+          const bool low = a.interleaved ? (i & 1) == 0 : c < h8;
           cs[i] = s_turn[wave][0][at], sn[i] = s_turn[wave][1][at];
+          if (low) sn[i] = -sn[i];
         }
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
     }
     const int64_t row0 = (int64_t(p.bad ? 0 : p.page) * ca.heads << ca.page_shift) + max(p.off, 0);
-    for (int t = first; t < last; ++t) {
-      const int seg = t < nq ? 0 : (t < nq + nkv ? 1 : 2);  // queries, keys, values
-      const int head = (t - (seg == 0 ? 0 : (seg == 1 ? nq : nq + nkv))) * heads + hl;
-      if (hl >= heads || head >= (seg == 0 ? a.q_heads : ca.heads)) continue;
-      if (seg != 0 && (none || p.bad)) continue;
-      float x[8];
+    // A task's head and values (and the other halves of its pairs), the next task's
+    // on their way while one is turned and stored.
+    struct Task {
+      int seg, head;  // queries, keys, values
+      bool some;
+      float x[8], y[8];
+    };
+    const auto fetch = [&](int t, Task& k) {
+      k.seg = t < nq ? 0 : (t < nq + nkv ? 1 : 2);
+      k.head = (t - (k.seg == 0 ? 0 : (k.seg == 1 ? nq : nq + nkv))) * heads + hl;
+      k.some = t < last && hl < heads && k.head < (k.seg == 0 ? a.q_heads : ca.heads) && (k.seg == 0 || !(none || p.bad));
+      if (!k.some || none) return;
+      const char* src = k.seg == 0 ? a.q + int64_t(r) * a.q_stride : ca.dense[k.seg - 1] + int64_t(r) * ca.stride[k.seg - 1];
+      src += (k.head * ca.dim + 8 * c) * kSize;
+      load8<TYPE>(src, k.x);
+      if (turned && k.seg != 2 && !a.interleaved) load8<TYPE>(src + other * (8 * kSize), k.y);
+    };
+    const auto finish = [&](Task& k) {
+      if (!k.some) return;
       if (none) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = p.bad_len ? __builtin_nanf("") : 0.0f;
-      } else {
-        const char* src = seg == 0 ? a.q + int64_t(r) * a.q_stride : ca.dense[seg - 1] + int64_t(r) * ca.stride[seg - 1];
-        src += (int64_t(head) * ca.dim + 8 * c) * kSize;
-        load8<TYPE>(src, x);
-        if (turned && seg != 2) {
-          float y[8];
-          if (a.interleaved) {
+        for (int i = 0; i < 8; ++i) k.x[i] = p.bad_len ? __builtin_nanf("") : 0.0f;
+      } else if (turned && k.seg != 2) {
+        if (a.interleaved) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = x[i ^ 1];
-          } else {
-            load8<TYPE>(src + other * 8 * kSize, y);
-          }
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const bool low = a.interleaved ? (i & 1) == 0 : c < h8;
-            x[i] = x[i] * cs[i] + (low ? -y[i] : y[i]) * sn[i];
-          }
+          for (int i = 0; i < 8; ++i) k.y[i] = k.x[i ^ 1];
         }
+        // (the sines of the pairs' first halves are negated)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) k.x[i] = k.x[i] * cs[i] + k.y[i] * sn[i];
       }
-      if (seg == 0) {
+      if (k.seg == 0) {
         char* dst = a.q_out + int64_t(r) * a.q_out_stride;
-        const int64_t at = int64_t(head) * ca.dim + 8 * c;
-        if (a.q_out_type == QTEA_F16) store8<QTEA_F16>(dst + at * 2, x);
-        else if (a.q_out_type == QTEA_BF16) store8<QTEA_BF16>(dst + at * 2, x);
-        else store8<QTEA_F32>(dst + at * 4, x);
+        const int at = k.head * ca.dim + 8 * c;
+        if (a.q_out_type == QTEA_F16) store8<QTEA_F16>(dst + at * 2, k.x);
+        else if (a.q_out_type == QTEA_BF16) store8<QTEA_BF16>(dst + at * 2, k.x);
+        else store8<QTEA_F32>(dst + at * 4, k.x);
       } else {
-        store_cached<FMT>(ca, seg - 1, row0 + (int64_t(head) << ca.page_shift), c, x);
+        store_cached<FMT>(ca, k.seg - 1, row0 + (int64_t(k.head) << ca.page_shift), c, k.x);
       }
+    };
+    Task even, odd;
+    fetch(first, even);
+    for (int t = first; t < last; t += 2) {
+      fetch(t + 1, odd);
+      finish(even);
+      fetch(t + 2, even);
+      finish(odd);
     }
   }
 }
@@ -342,7 +361,11 @@ int qtea_kv_append_rotated(const qtea_kv_cache* cache, const qtea_kv_batch* batc
   if (a.c.b.n_tokens == 0) return QTEA_OK;
   const int heads = 64 / (cache->head_dim / 8);
   a.tasks = (n_q_heads + heads - 1) / heads + 2 * ((cache->n_heads + heads - 1) / heads);
-  a.per_part = a.tasks, a.parts = 1;
+  // Tasks a wave: all of a token's, or where that leaves the chip without waves
+  // (eight a CU of 256) as few as fill it: 16 tokens of 12 tasks 4.0 us at one,
+  // 9.1 at twelve; 19500 tokens 228 us at one, 117 at twelve.
+  a.per_part = int32_t(std::min<int64_t>(a.tasks, std::max<int64_t>(1, int64_t(a.tasks) * a.c.b.n_tokens / kFullWaves)));
+  a.parts = (a.tasks + a.per_part - 1) / a.per_part;
   const int64_t blocks = std::min<int64_t>((int64_t(a.c.b.n_tokens) * a.parts + kThreads / 64 - 1) / (kThreads / 64), 1 << 20);
   for_kernel(cache->format, type, [&](auto fmt, auto ty) {
     hipLaunchKernelGGL((kv_append_rotated_kernel<decltype(fmt)::value, decltype(ty)::value>), dim3(uint32_t(blocks)), dim3(kThreads), 0,
