@@ -124,7 +124,7 @@ struct RotateArgs {
   char* q_out;
   int64_t q_stride, q_out_stride;  // bytes
   const float* freq;
-  int32_t q_heads, rot, interleaved, q_out_type;
+  int32_t q_heads, rot, q_out_type;
   int32_t tasks, parts, per_part;  // tasks of a token, waves that share them, tasks a wave
 };
 
@@ -149,7 +149,7 @@ __device__ __forceinline__ void turn_of(int pos, float freq, float& cs, float& s
   if (quarter == 1 || quarter == 2) cs = -cs;
 }
 
-template <int FMT, int TYPE>
+template <int FMT, int TYPE, bool INTERLEAVED, int AHEAD>
 __global__ __launch_bounds__(kThreads) void kv_append_rotated_kernel(const RotateArgs a) {
   __shared__ float s_turn[kThreads / 64][2][kMaxAngles];
   const CacheArgs& ca = a.c;
@@ -160,13 +160,40 @@ __global__ __launch_bounds__(kThreads) void kv_append_rotated_kernel(const Rotat
   const int nq = (a.q_heads + heads - 1) / heads, nkv = (ca.heads + heads - 1) / heads;
   const int half = a.rot / 2, h8 = a.rot / 16;
   const bool turned = 8 * c < a.rot;
-  const int other = c < h8 ? h8 : -h8;  // octs to the pairs' other halves
+  const int other = INTERLEAVED || !turned ? 0 : (c < h8 ? h8 : -h8);  // octs to the pairs' other halves
   const int64_t waves = int64_t(ca.b.n_tokens) * a.parts;
   for (int64_t w0 = int64_t(blockIdx.x) * (kThreads / 64); w0 < waves; w0 += int64_t(gridDim.x) * (kThreads / 64)) {
     const int w = __builtin_amdgcn_readfirstlane(int(w0) + wave);
     const int r = w / a.parts, part = w - r * a.parts;
     if (r >= ca.b.n_tokens) return;
     const int first = part * a.per_part, last = min(first + a.per_part, a.tasks);
+
+    // A task's values and the other halves of their pairs, on their way while the tasks
+    // before it are turned and stored.  Every lane loads, whatever is stored (the
+    // last head again, or past the wave's tasks the token's first key): a
+    // number of loads that does not depend on the call lets the wave wait for the
+    // one it needs.
+    struct Task {
+      int seg, head;  // queries, keys, values
+      Raw<TYPE> x, y;
+    };
+    const char* const rows[3] = {a.q + int64_t(r) * a.q_stride, ca.dense[0] + int64_t(r) * ca.stride[0], ca.dense[1] + int64_t(r) * ca.stride[1]};
+    const auto fetch = [&](int t) {
+      Task k;
+      k.seg = t < nq ? 0 : (t < nq + nkv ? 1 : 2);
+      k.head = (t - (k.seg == 0 ? 0 : (k.seg == 1 ? nq : nq + nkv))) * heads + hl;
+      const char* row = k.seg == 0 ? rows[0] : (k.seg == 1 ? rows[1] : rows[2]);
+      const int at = min(k.head, (k.seg == 0 ? a.q_heads : ca.heads) - 1) * ca.dim + 8 * c;
+      const bool in = t < last;
+      row = in ? row : rows[1];
+      k.x = load_raw<TYPE>(row + (in ? at * kSize : 0));
+      if constexpr (!INTERLEAVED) k.y = load_raw<TYPE>(row + (in ? (at + 8 * other) * kSize : 0));
+      return k;
+    };
+    Task task[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) task[i] = fetch(first + i);
+
     const Place p = place_of(ca, r);
     if (!p.some) continue;
     const bool none = p.bad_len || p.pos < 0;
@@ -176,68 +203,53 @@ __global__ __launch_bounds__(kThreads) void kv_append_rotated_kernel(const Rotat
       // (a wave's LDS accesses are made in order; only the compiler has to keep it)
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
-      const int base = a.interleaved ? 4 * c : (c < h8 ? 8 * c : 8 * c - half);
-      if (turned) {
+      const int base = INTERLEAVED ? 4 * c : (c < h8 ? 8 * c : 8 * c - half);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int at = base + (a.interleaved ? i / 2 : i);
-          const bool low = a.interleaved ? (i & 1) == 0 : c < h8;
-          cs[i] = s_turn[wave][0][at], sn[i] = s_turn[wave][1][at];
-          if (low) sn[i] = -sn[i];
-        }
+      for (int i = 0; i < 8; ++i) {
+        const int at = turned ? base + (INTERLEAVED ? i / 2 : i) : 0;
+        const bool low = INTERLEAVED ? (i & 1) == 0 : c < h8;
+        const float s = s_turn[wave][1][at];
+        cs[i] = turned ? s_turn[wave][0][at] : 1.0f;
+        sn[i] = !turned ? 0.0f : (low ? -s : s);  // (negated for the pairs' first halves)
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
     }
     const int64_t row0 = (int64_t(p.bad ? 0 : p.page) * ca.heads << ca.page_shift) + max(p.off, 0);
-    // A task's head and values (and the other halves of its pairs), the next task's
-    // on their way while one is turned and stored.
-    struct Task {
-      int seg, head;  // queries, keys, values
-      bool some;
-      float x[8], y[8];
-    };
-    const auto fetch = [&](int t, Task& k) {
-      k.seg = t < nq ? 0 : (t < nq + nkv ? 1 : 2);
-      k.head = (t - (k.seg == 0 ? 0 : (k.seg == 1 ? nq : nq + nkv))) * heads + hl;
-      k.some = t < last && hl < heads && k.head < (k.seg == 0 ? a.q_heads : ca.heads) && (k.seg == 0 || !(none || p.bad));
-      if (!k.some || none) return;
-      const char* src = k.seg == 0 ? a.q + int64_t(r) * a.q_stride : ca.dense[k.seg - 1] + int64_t(r) * ca.stride[k.seg - 1];
-      src += (k.head * ca.dim + 8 * c) * kSize;
-      load8<TYPE>(src, k.x);
-      if (turned && k.seg != 2 && !a.interleaved) load8<TYPE>(src + other * (8 * kSize), k.y);
-    };
-    const auto finish = [&](Task& k) {
-      if (!k.some) return;
+    const auto finish = [&](const Task& k) {
+      if (hl >= heads || k.head >= (k.seg == 0 ? a.q_heads : ca.heads) || (k.seg != 0 && (none || p.bad))) return;
+      float x[8];
+      values<TYPE>(k.x, x);
       if (none) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) k.x[i] = p.bad_len ? __builtin_nanf("") : 0.0f;
-      } else if (turned && k.seg != 2) {
-        if (a.interleaved) {
+        for (int i = 0; i < 8; ++i) x[i] = p.bad_len ? __builtin_nanf("") : 0.0f;
+      } else if (k.seg != 2 && turned) {
+        float y[8];
+        if constexpr (INTERLEAVED) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) k.y[i] = k.x[i ^ 1];
+          for (int i = 0; i < 8; ++i) y[i] = x[i ^ 1];
+        } else {
+          values<TYPE>(k.y, y);
         }
-        // (the sines of the pairs' first halves are negated)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) k.x[i] = k.x[i] * cs[i] + k.y[i] * sn[i];
+        for (int i = 0; i < 8; ++i) x[i] = x[i] * cs[i] + y[i] * sn[i];
       }
       if (k.seg == 0) {
         char* dst = a.q_out + int64_t(r) * a.q_out_stride;
         const int at = k.head * ca.dim + 8 * c;
-        if (a.q_out_type == QTEA_F16) store8<QTEA_F16>(dst + at * 2, k.x);
-        else if (a.q_out_type == QTEA_BF16) store8<QTEA_BF16>(dst + at * 2, k.x);
-        else store8<QTEA_F32>(dst + at * 4, k.x);
+        if (a.q_out_type == QTEA_F16) store8<QTEA_F16>(dst + at * 2, x);
+        else if (a.q_out_type == QTEA_BF16) store8<QTEA_BF16>(dst + at * 2, x);
+        else store8<QTEA_F32>(dst + at * 4, x);
       } else {
-        store_cached<FMT>(ca, k.seg - 1, row0 + (int64_t(k.head) << ca.page_shift), c, k.x);
+        store_cached<FMT>(ca, k.seg - 1, row0 + (int64_t(k.head) << ca.page_shift), c, x);
       }
     };
-    Task even, odd;
-    fetch(first, even);
-    for (int t = first; t < last; t += 2) {
-      fetch(t + 1, odd);
-      finish(even);
-      fetch(t + 2, even);
-      finish(odd);
+    for (int t = first; t < last; t += AHEAD) {
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        if (t + i < last) finish(task[i]);
+        task[i] = fetch(t + i + AHEAD);
+      }
     }
   }
 }
@@ -357,19 +369,24 @@ int qtea_kv_append_rotated(const qtea_kv_cache* cache, const qtea_kv_batch* batc
   }
   a.q = static_cast<const char*>(q), a.q_out = static_cast<char*>(q_out);
   a.q_stride = q_stride * elem_bytes(type), a.q_out_stride = q_out_stride * elem_bytes(q_out_type);
-  a.freq = freq, a.q_heads = n_q_heads, a.rot = rot_dim, a.interleaved = interleaved != 0, a.q_out_type = q_out_type;
+  a.freq = freq, a.q_heads = n_q_heads, a.rot = rot_dim, a.q_out_type = q_out_type;
   if (a.c.b.n_tokens == 0) return QTEA_OK;
   const int heads = 64 / (cache->head_dim / 8);
   a.tasks = (n_q_heads + heads - 1) / heads + 2 * ((cache->n_heads + heads - 1) / heads);
   // Tasks a wave: all of a token's, or where that leaves the chip without waves
   // (eight a CU of 256) as few as fill it: 16 tokens of 12 tasks 4.0 us at one,
-  // 9.1 at twelve; 19500 tokens 228 us at one, 117 at twelve.
+  // 9.1 at twelve; 19500 tokens 228 us at one, 117 at twelve
+  // (before tasks were loaded ahead).
   a.per_part = int32_t(std::min<int64_t>(a.tasks, std::max<int64_t>(1, int64_t(a.tasks) * a.c.b.n_tokens / kFullWaves)));
   a.parts = (a.tasks + a.per_part - 1) / a.per_part;
   const int64_t blocks = std::min<int64_t>((int64_t(a.c.b.n_tokens) * a.parts + kThreads / 64 - 1) / (kThreads / 64), 1 << 20);
   for_kernel(cache->format, type, [&](auto fmt, auto ty) {
-    hipLaunchKernelGGL((kv_append_rotated_kernel<decltype(fmt)::value, decltype(ty)::value>), dim3(uint32_t(blocks)), dim3(kThreads), 0,
-                       static_cast<hipStream_t>(stream), a);
+    constexpr int F = decltype(fmt)::value, T = decltype(ty)::value;
+    // (three tasks on the way where a wave has more than one: 19500 tokens 100.5 us,
+    // 104 with two, 117 with none)
+    const auto kernel = a.per_part > 1 ? (interleaved ? kv_append_rotated_kernel<F, T, true, 3> : kv_append_rotated_kernel<F, T, false, 3>)
+                                       : (interleaved ? kv_append_rotated_kernel<F, T, true, 1> : kv_append_rotated_kernel<F, T, false, 1>);
+    hipLaunchKernelGGL(kernel, dim3(uint32_t(blocks)), dim3(kThreads), 0, static_cast<hipStream_t>(stream), a);
   });
   return hipGetLastError() == hipSuccess ? QTEA_OK : QTEA_ERR_HIP;
 }

@@ -40,6 +40,38 @@ __device__ __forceinline__ void store8(char* p, const float (&x)[8]) {
   }
 }
 
+// 8 values as they are loaded, from a row that is read for the last time.
+constexpr int kNone = -1;  // in the place of a type: no such operand
+template <int T>
+struct Raw {
+  u32x4 v[T == QTEA_F32 ? 2 : 1];
+};
+template <>
+struct Raw<kNone> {};
+
+template <int T>
+__device__ __forceinline__ Raw<T> load_raw(const char* p) {
+  Raw<T> r;
+  const u32x4* q = reinterpret_cast<const u32x4*>(p);
+  r.v[0] = __builtin_nontemporal_load(q);
+  if constexpr (T == QTEA_F32) r.v[1] = __builtin_nontemporal_load(q + 1);
+  return r;
+}
+template <int T>
+__device__ __forceinline__ void values(const Raw<T>& r, float (&x)[8]) {
+  if constexpr (T == QTEA_F32) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(r.v[i / 4][i & 3]);
+  } else if constexpr (T == QTEA_F16) {
+    const half8_t h = __builtin_bit_cast(half8_t, r.v[0]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = float(h[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(r.v[0][i] << 16), x[2 * i + 1] = __uint_as_float(r.v[0][i] & 0xffff0000u);
+  }
+}
+
 // One value, aligned to itself.
 template <int TYPE>
 __device__ __forceinline__ float load1(const char* p) {
