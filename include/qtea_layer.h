@@ -113,7 +113,8 @@ int qtea_w4_unpack(const void* packed, int64_t packed_bytes, int64_t N, int64_t 
  *   X        device [batch][K] of x_type (QTEA_F16, QTEA_BF16 or QTEA_E4M3),
  *            x_stride elements from row to row (>= K), aligned to its elements.
  *            QTEA_E4M3: K a multiple of 32, X 16-byte aligned, x_stride a
- *            multiple of 16
+ *            multiple of 16.  From the first row's start to the last one's end
+ *            at most 2^30 bytes (x_scale too)
  *   x_scale  device uint8 [batch][K / 32], x_scale_stride bytes from row to
  *            row (QTEA_E4M3; NULL otherwise)
  *   Y        device [batch][N] of y_type (enum qtea_type), y_stride elements

@@ -17,9 +17,10 @@
 namespace qtea_serve {
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 512, kWaves = kThreads / 64;
 constexpr int kTile = 1024;       // bytes of a tile's codes
 constexpr int kUnitScales = 256;  // bytes of four tiles' scales
+constexpr int kWideStrips = 4;    // strips of a wave where there are many
 
 struct Layout {
   int64_t strips, tiles, units, scales_at, bytes;  // of 16 rows; tiles and units of four tiles of a strip
@@ -197,11 +198,13 @@ constexpr uint32_t kPastEnd = 0x80000000u;  // an offset past every descriptor's
 template <int XT, bool ODD>
 __device__ __forceinline__ Piece<XT> load_piece(const GemmArgs& a, const XBuf& xb, int row, int k) {
   Piece<XT> r;
-  const bool in = k < a.K && row < a.batch;
-  const uint32_t at = in ? uint32_t(k) * elem_bytes(XT) : kPastEnd, row_at = uint32_t(row) * uint32_t(a.x_stride);
+  // (a row past the batch: a scalar offset past the end would not be the
+  // descriptor's to refuse)
+  const bool row_in = row < a.batch, in = row_in && k < a.K;
+  const uint32_t at = in ? uint32_t(k) * elem_bytes(XT) : kPastEnd, row_at = row_in ? uint32_t(row) * uint32_t(a.x_stride) : 0u;
   if constexpr (XT == QTEA_E4M3) {  // (K is a multiple of 32)
     r.v = __builtin_amdgcn_raw_buffer_load_b64(xb.x, at, row_at, 0);
-    r.scale = uint8_t(__builtin_amdgcn_raw_buffer_load_b8(xb.scale, in ? uint32_t(k) / 32 : kPastEnd, uint32_t(row) * uint32_t(a.x_scale_stride), 0));
+    r.scale = uint8_t(__builtin_amdgcn_raw_buffer_load_b8(xb.scale, in ? uint32_t(k) / 32 : kPastEnd, row_in ? uint32_t(row) * uint32_t(a.x_scale_stride) : 0u, 0));
   } else if constexpr (!ODD) {
     r.v = __builtin_amdgcn_raw_buffer_load_b128(xb.x, at, row_at, 0);
   } else {
@@ -253,7 +256,7 @@ __global__ __launch_bounds__(kThreads) void w4_gemm_split_kernel(const GemmArgs 
   extern __shared__ u32x4 s_x[];  // [waves][4 tiles * 4 * 64]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), q = lane >> 4;
   const int part = wave % a.parts;
-  const int64_t group = int64_t(blockIdx.x) * (kThreads / 64 / a.parts) + wave / a.parts;
+  const int64_t group = int64_t(blockIdx.x) * (kWaves / a.parts) + wave / a.parts;
   const int64_t strip0 = min(group * R, int64_t(a.strips) - R);  // (the last groups: strips of others, again)
   const int row0 = blockIdx.y * 16;
   const XBuf xb = x_buffers<XT>(a);
@@ -348,25 +351,30 @@ __global__ __launch_bounds__(kThreads) void w4_gemm_split_kernel(const GemmArgs 
   }
 }
 
-// Many strips: a workgroup's waves take R strips each over all columns, and share
-// the activations in LDS, a unit (512 columns) at a time, two units there: the
-// next one is loaded while this one is multiplied, one barrier a unit.
-template <int XT, int R, int CT, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void w4_gemm_wide_kernel(const GemmArgs a) {
+// Many strips: four a wave, its operands from LDS serve all of them.  A workgroup's waves
+// share the activations there, a unit (512 columns) at a time, two units there: the
+// next one is loaded while this one is multiplied, one barrier a unit.  PARTS waves
+// share their strips, each has a tile or two of every unit's four, and their
+// sums are added at the end: so a workgroup has four strips a wave to keep LDS
+// idle enough, and as few strips altogether as give every CU its share.
+template <int XT, int CT, int PARTS>
+__global__ __launch_bounds__(kThreads) void w4_gemm_wide_kernel(const GemmArgs a) {
   using T = Type<XT>;
-  constexpr int AHEAD = R == 4 ? 1 : 2;        // units of codes on the way
-  constexpr int ROWS = CT * 16 / WAVES;        // rows of X a wave brings
+  constexpr int R = kWideStrips, TILES = 4 / PARTS;  // strips of a wave, tiles of a unit
+  constexpr int AHEAD = PARTS == 1 || (PARTS == 2 && CT > 2) ? 1 : 2;  // units of codes on the way, 8 or 16 KB a wave (as registers allow)
+  constexpr int ROWS = CT * 16 / kWaves;             // rows of X a wave brings
   extern __shared__ u32x4 s_x[];  // [2][4 tiles * CT * 4 * 64]
   constexpr int kBuf = 4 * CT * 4 * 64;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), q = lane >> 4;
-  const int64_t strip0 = min((int64_t(blockIdx.x) * WAVES + wave) * R, int64_t(a.strips) - R);  // (the last waves: strips of others, again)
+  const int part = wave % PARTS, tile0 = part * TILES;
+  const int64_t strip0 = min((int64_t(blockIdx.x) * (kWaves / PARTS) + wave / PARTS) * R, int64_t(a.strips) - R);  // (the last waves: strips of others, again)
   const uint8_t* codes = a.codes + strip0 * kTile;
   const uint8_t* scales = a.scales + strip0 * kUnitScales;
   const XBuf xb = x_buffers<XT>(a);
-  u32x4 w[AHEAD][4][R];
+  u32x4 w[AHEAD][TILES][R];
   uint32_t sc[AHEAD][R];
   auto load = [&](int s, int u, int j) {
-    const uint64_t p = scalar(codes + int64_t(min(4 * u + j, a.tiles - 1)) * a.strips * kTile);  // (past the last tile: that one again, times zeros)
+    const uint64_t p = scalar(codes + int64_t(min(4 * u + tile0 + j, a.tiles - 1)) * a.strips * kTile);  // (past the last tile: that one again, times zeros)
 #pragma unroll
     for (int r = 0; r < R; ++r) w[s][j][r] = load_codes(p, lane, r);
   };
@@ -376,15 +384,15 @@ __global__ __launch_bounds__(64 * WAVES) void w4_gemm_wide_kernel(const GemmArgs
     for (int r = 0; r < R; ++r) sc[s][r] = load_scale4(p, lane, r);
   };
   // A wave brings whole rows of a unit, 8 columns a lane.
-  Piece<XT> x[ROWS];
-  auto load_x = [&](int u) {
+  Piece<XT> x[AHEAD][ROWS];
+  auto load_x = [&](int s, int u) {
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) x[i] = load_piece<XT, false>(a, xb, i * WAVES + wave, u * 512 + lane * 8);
+    for (int i = 0; i < ROWS; ++i) x[s][i] = load_piece<XT, false>(a, xb, i * kWaves + wave, u * 512 + lane * 8);
   };
-  auto write_x = [&](int u) {
+  auto write_x = [&](int s, int u) {
     const int at = fresh(lane);
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) s_x[(u & 1) * kBuf + piece_to<CT>(i * WAVES + wave, at)] = piece_value<XT>(a, x[i], u * 512 + lane * 8);
+    for (int i = 0; i < ROWS; ++i) s_x[(u & 1) * kBuf + piece_to<CT>(i * kWaves + wave, at)] = piece_value<XT>(a, x[s][i], u * 512 + lane * 8);
   };
   f32x4 c[CT][R];
 #pragma unroll
@@ -392,63 +400,94 @@ __global__ __launch_bounds__(64 * WAVES) void w4_gemm_wide_kernel(const GemmArgs
 #pragma unroll
     for (int r = 0; r < R; ++r) c[t][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-  load_x(0);
+  // A wave's loads arrive in order, so the activations of a unit are asked for right
+  // after the codes of the unit before it: whoever waits for them has those already.
+  load_x(0, 0);
 #pragma unroll
   for (int s = 0; s < AHEAD; ++s) {
     load_scales(s, s);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      load(s, s, j);
-      __builtin_amdgcn_sched_barrier(0);
-    }
+    for (int j = 0; j < TILES; ++j) load(s, s, j);
+    __builtin_amdgcn_sched_barrier(0);
+    if (s == 0) write_x(0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    load_x((s + 1) % AHEAD, s + 1);
+    __builtin_amdgcn_sched_barrier(0);
   }
-  write_x(0);
   __syncthreads();
   for (int u0 = 0; u0 < a.units; u0 += AHEAD) {
 #pragma unroll
     for (int s = 0; s < AHEAD; ++s) {
       const int u = u0 + s;
       if (u >= a.units) break;
-      load_x(u + 1);
-      __builtin_amdgcn_sched_barrier(0);
       const u32x4* buf = s_x + (u & 1) * kBuf;
       u32x4 B[2][CT];
       auto read_x = [&](int step) {
         const int at = fresh(lane);
 #pragma unroll
-        for (int t = 0; t < CT; ++t) B[step & 1][t] = buf[piece_at<CT>(step / 4, t, step & 3, at)];
+        for (int t = 0; t < CT; ++t) B[step & 1][t] = buf[piece_at<CT>(tile0 + step / 4, t, step & 3, at)];
+      };
+      u32x4 A[2][R];
+      auto decode = [&](int step) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) A[step & 1][r] = weights<T>(w[s][step / 4][r][step & 3], scale_of(sc[s][r] >> (8 * (tile0 + step / 4)) & 255u));
       };
       read_x(0);
+      decode(0);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float f[R];
-#pragma unroll
-        for (int r = 0; r < R; ++r) f[r] = scale_of(sc[s][r] >> (8 * j) & 255u);
+      for (int j = 0; j < TILES; ++j) {
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
-          if (j < 3 || m < 3) read_x(4 * j + m + 1);  // the next instructions' right operands, a step ahead
+          const int step = 4 * j + m;
           __builtin_amdgcn_sched_barrier(0);
-          u32x4 A[R];
-#pragma unroll
-          for (int r = 0; r < R; ++r) A[r] = weights<T>(w[s][j][r][m], f[r]);
+          if (step + 1 < 4 * TILES) read_x(step + 1), decode(step + 1);
 #pragma unroll
           for (int t = 0; t < CT; ++t)
 #pragma unroll
-            for (int r = 0; r < R; ++r) c[t][r] = T::mfma16(A[r], B[m & 1][t], c[t][r]);
+            for (int r = 0; r < R; ++r) c[t][r] = T::mfma16(A[step & 1][r], B[step & 1][t], c[t][r]);
+          // the next step's operands between this one's products
+          __builtin_amdgcn_sched_group_barrier(0x100, CT, 0);
+#pragma unroll
+          for (int i = 0; i < CT * R; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x2, (20 + CT * R - 1) / (CT * R), 0);
+          }
         }
         __builtin_amdgcn_sched_barrier(0);
         load(s, u + AHEAD, j);
         __builtin_amdgcn_sched_barrier(0);
       }
       load_scales(s, u + AHEAD);
-      if (u + 1 < a.units) write_x(u + 1);
+      write_x((s + 1) % AHEAD, u + 1);  // (past the last unit: zeros)
+      load_x((s + 1) % AHEAD, u + 1 + AHEAD);
       __syncthreads();
     }
   }
+  if constexpr (PARTS > 1) {
+    // the parts' sums, in order (LDS has room for all: 4 CT KB a wave)
+    f32x4* sums = reinterpret_cast<f32x4*>(s_x);  // [waves][CT][R][64]
 #pragma unroll
-  for (int t = 0; t < CT; ++t)
+    for (int t = 0; t < CT; ++t)
 #pragma unroll
-    for (int r = 0; r < R; ++r) store_y(a, t * 16 + (lane & 15), (strip0 + r) * 16 + 4 * q, c[t][r]);
+      for (int r = 0; r < R; ++r) sums[((wave * CT + t) * R + r) * 64 + lane] = c[t][r];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < R / PARTS; ++i) {
+      const int r = i * PARTS + part;
+#pragma unroll
+      for (int t = 0; t < CT; ++t) {
+        f32x4 sum = sums[(((wave - part) * CT + t) * R + r) * 64 + lane];
+#pragma unroll
+        for (int k = 1; k < PARTS; ++k) sum += sums[(((wave - part + k) * CT + t) * R + r) * 64 + lane];
+        store_y(a, t * 16 + (lane & 15), (strip0 + r) * 16 + 4 * q, sum);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int t = 0; t < CT; ++t)
+#pragma unroll
+      for (int r = 0; r < R; ++r) store_y(a, t * 16 + (lane & 15), (strip0 + r) * 16 + 4 * q, c[t][r]);
+  }
 }
 
 }  // namespace
@@ -487,14 +526,13 @@ int compute_units() {
 
 using std::integral_constant;
 
-template <int XT, int R, int CT, int WAVES>
+template <int XT, int CT, int PARTS>
 int run_wide(const GemmArgs& a, hipStream_t st) {
-  const auto kernel = w4_gemm_wide_kernel<XT, R, CT, WAVES>;
+  const auto kernel = w4_gemm_wide_kernel<XT, CT, PARTS>;
   static std::atomic<int> allowed[qtea_detail::kMaxDevices];
-  constexpr int lds = 2 * 4 * CT * 4 * 64 * 16;
+  constexpr int lds = 2 * 4 * CT * 4 * 64 * 16, strips = kWideStrips * kWaves / PARTS;
   if (qtea_detail::allow_lds(reinterpret_cast<const void*>(kernel), lds, allowed) != hipSuccess) return QTEA_ERR_HIP;
-  const int64_t blocks = (int64_t(a.strips) + R * WAVES - 1) / (R * WAVES);
-  hipLaunchKernelGGL(kernel, dim3(uint32_t(blocks)), dim3(64 * WAVES), lds, st, a);
+  hipLaunchKernelGGL(kernel, dim3(uint32_t((int64_t(a.strips) + strips - 1) / strips)), dim3(kThreads), lds, st, a);
   return hipGetLastError() == hipSuccess ? QTEA_OK : QTEA_ERR_HIP;
 }
 
@@ -502,10 +540,10 @@ template <int XT, int R, int ROWS, bool ODD>
 int run_split(const GemmArgs& a, hipStream_t st) {
   const auto kernel = w4_gemm_split_kernel<XT, R, ROWS, ODD>;
   static std::atomic<int> allowed[qtea_detail::kMaxDevices];
-  constexpr int lds = kThreads / 64 * 4 * 4 * 64 * 16;
+  constexpr int lds = kWaves * 4 * 4 * 64 * 16;
   if (qtea_detail::allow_lds(reinterpret_cast<const void*>(kernel), lds, allowed) != hipSuccess) return QTEA_ERR_HIP;
   const int64_t groups = (int64_t(a.strips) + R - 1) / R;
-  const int per = kThreads / 64 / a.parts;
+  const int per = kWaves / a.parts;
   hipLaunchKernelGGL(kernel, dim3(uint32_t((groups + per - 1) / per), uint32_t((a.batch + 15) / 16)), dim3(kThreads), lds, st, a);
   return hipGetLastError() == hipSuccess ? QTEA_OK : QTEA_ERR_HIP;
 }
@@ -519,23 +557,20 @@ template <int XT>
 int run_gemm(GemmArgs a, int cus, hipStream_t st) {
   const int ct = (a.batch + 15) / 16;
   if (a.x_dwords && a.strips >= (ct == 1 ? 5 : 3) * cus) {
-    // Strips and waves of a workgroup: the fewest strips on the CU that has most,
-    // then the most a workgroup (a wave's operands from LDS serve all its strips:
-    // 128257 x 4096 at 64 rows 71 us with four, 86 with two, 110 with one).  Past 32
-    // rows one workgroup fills a CU's LDS and has eight waves.
-    int R = 1, waves = 8;
+    // Strips of a workgroup: the fewest on the CU that has most, then the most.  (57344
+    // x 8192 at 16 rows, 14 strips a CU: 48.7 us with workgroups of 8 strips, 44.5
+    // of 16, 56.9 of 32; 28672 x 4096, 7 a CU: 13.3, 17.0, 23.4.)
+    int strips = 0;
     int64_t least = INT64_MAX;
-    for (int r = 1; r <= 4; r *= 2)
-      for (int w = 8; w >= (r == 4 || ct > 2 ? 8 : 4); w -= 4) {
-        const int64_t blocks = (int64_t(a.strips) + r * w - 1) / (r * w), most = (blocks + cus - 1) / cus * r * w;
-        if (most < least || (most == least && r * w > R * waves)) least = most, R = r, waves = w;
-      }
+    for (const int n : {32, 16, 8}) {
+      const int64_t blocks = (int64_t(a.strips) + n - 1) / n, most = (blocks + cus - 1) / cus * n;
+      if (most < least && (n == 32 || blocks < (1 << 22))) least = most, strips = n;  // (a grid has 2^32 threads)
+    }
     const auto with = [&](auto cols) {
       constexpr int CT = decltype(cols)::value;
-      if (R == 4) return run_wide<XT, 4, CT, 8>(a, st);
-      if (waves == 8) return R == 2 ? run_wide<XT, 2, CT, 8>(a, st) : run_wide<XT, 1, CT, 8>(a, st);
-      if constexpr (CT <= 2) return R == 2 ? run_wide<XT, 2, CT, 4>(a, st) : run_wide<XT, 1, CT, 4>(a, st);
-      return int(QTEA_ERR_HIP);  // (not reached)
+      if (strips == 32) return run_wide<XT, CT, 1>(a, st);
+      if (strips == 16) return run_wide<XT, CT, 2>(a, st);
+      return run_wide<XT, CT, 4>(a, st);
     };
     if (ct == 1) return with(integral_constant<int, 1>());
     if (ct == 2) return with(integral_constant<int, 2>());
@@ -547,7 +582,7 @@ int run_gemm(GemmArgs a, int cus, hipStream_t st) {
   int R = a.x_dwords ? 4 : 2;
   while (R > 1 && (a.strips < R || int64_t(a.strips) * ct * 10 < int64_t(R) * 6 * cus)) R /= 2;
   a.parts = 1;
-  while (a.parts < kThreads / 64 && a.parts < a.units && (int64_t(a.strips) + R - 1) / R * a.parts < 8 * int64_t(cus)) a.parts *= 2;
+  while (a.parts < kWaves && a.parts < a.units && (int64_t(a.strips) + R - 1) / R * a.parts < 8 * int64_t(cus)) a.parts *= 2;
   const auto with = [&](auto strips) {
     constexpr int RR = decltype(strips)::value;
     if constexpr (XT != QTEA_E4M3 && RR < 4) {

@@ -30,20 +30,18 @@ def _tokens(t, what, device):
     part contiguous: the stride of its tokens (of one token it is not used,
     whatever the view has)."""
     shape, stride = t.shape, t.stride()
-    n = len(shape)
-    if n == 2:
-        run = shape[1]
-        if stride[1] != 1 and run > 1:
-            raise ValueError(f"{what}: a row's elements are contiguous")
-    elif n == 3:
-        run = shape[1] * shape[2]
-        if (stride[2] != 1 and shape[2] > 1) or (stride[1] != shape[2] and shape[1] > 1):
-            raise ValueError(f"{what}: a token's heads and elements are contiguous")
-    else:
-        raise ValueError(f"{what}: [rows][n] or [tokens][heads][n], got {list(shape)}")
     if t.get_device() != device:
         raise ValueError(f"{what}: a device tensor, a call's of one device")
-    return run if shape[0] <= 1 else stride[0]
+    n = len(shape)
+    if n == 2:
+        if stride[1] != 1 and shape[1] > 1:
+            raise ValueError(f"{what}: a row's elements are contiguous")
+        return stride[0] if shape[0] > 1 else shape[1]
+    if n != 3:
+        raise ValueError(f"{what}: [rows][n] or [tokens][heads][n], got {list(shape)}")
+    if (stride[2] != 1 and shape[2] > 1) or (stride[1] != shape[2] and shape[1] > 1):
+        raise ValueError(f"{what}: a token's heads and elements are contiguous")
+    return stride[0] if shape[0] > 1 else shape[1] * shape[2]
 
 
 def _scales(codes, scale, what):

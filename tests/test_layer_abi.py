@@ -59,7 +59,7 @@ def test_w4_refuses(lib):
         return lib.qtea_w4_gemm_lowbatch(p, nbytes, N, K, X, xt, xs, sc, ss, batch, Y, yt, ys, None)
 
     for change in (dict(p=None), dict(X=None), dict(Y=None), dict(p=VP((1 << 20) + 8)), dict(N=0), dict(K=0), dict(N=1 << 31), dict(K=(1 << 24) + 1), dict(xt=2), dict(xt=4),
-                   dict(xs=95), dict(X=ODD), dict(Y=ODD), dict(yt=3), dict(ys=99), dict(sc=ADDR), dict(xt=3), dict(xt=3, sc=ADDR, ss=2), dict(xt=3, sc=ADDR, ss=3, xs=104),
+                   dict(xs=95), dict(xs=1 << 29), dict(xt=3, sc=ADDR, ss=1 << 30), dict(X=ODD), dict(Y=ODD), dict(yt=3), dict(ys=99), dict(sc=ADDR), dict(xt=3), dict(xt=3, sc=ADDR, ss=2), dict(xt=3, sc=ADDR, ss=3, xs=104),
                    dict(xt=3, sc=ADDR, ss=3, X=VP((1 << 21) + 8)), dict(xt=3, sc=ADDR, ss=3, K=90)):
         assert gemm(**change) == BAD, change
     assert gemm(batch=0) == gemm(batch=65) == q.QTEA_ERR_BATCH
