@@ -120,7 +120,8 @@ int qtea_w4_unpack(const void* packed, int64_t packed_bytes, int64_t N, int64_t 
  *   Y        device [batch][N] of y_type (enum qtea_type), y_stride elements
  *            from row to row (>= N), aligned to its elements
  * Products are exact, sums fp32, one rounding to y_type.  A row of X reaches
- * its own row of Y only.
+ * its own row of Y only.  (E4M3 activations are multiplied as bf16 values: exact
+ * for scale bytes 10..246, that is wherever those are normal numbers.)
  * Errors: QTEA_ERR_INVALID_ARG, QTEA_ERR_BATCH, QTEA_ERR_WORKSPACE (a packed
  * buffer too small), QTEA_ERR_HIP.
  */

@@ -20,7 +20,7 @@ import torch
 
 import paper_2609_00224_amd as _q
 from paper_2609_00224_amd import QTEA_E4M3
-from paper_2609_00224_amd.serving import _call, _type
+from paper_2609_00224_amd.serving import _TYPES, _call, _type
 
 _U8 = torch.uint8
 
@@ -53,11 +53,13 @@ def _scales(codes, scale, what):
 
 def _out(out, out_scale, device):
     """An output's type, stride, scales and their stride."""
-    stride = _tokens(out, "out", device)
-    if out.dtype is not _U8:
+    stride, kind = _tokens(out, "out", device), _TYPES.get(out.dtype)
+    if kind is not None:
         if out_scale is not None:
             raise ValueError("out_scale: for 8-bit outputs only")
-        return _type(out, "out"), stride, None, 0
+        return kind, stride, None, 0
+    if out.dtype is not _U8:
+        raise ValueError(f"out: fp16, bf16, fp32 or uint8 codes, got {out.dtype}")
     if out.shape[-1] % 32:
         raise ValueError("out: 8-bit rows are a multiple of 32 long")
     return QTEA_E4M3, stride, *_scales(out, out_scale, "out_scale")
@@ -78,11 +80,11 @@ def qtea_rms_norm(x, weight, out, residual=None, eps: float = 1e-6, out_scale=No
     rs, rt, rp = (0, 0, None) if residual is None else (_tokens(residual, "residual", dev), _type(residual, "residual"), residual.data_ptr())
     wt, wp = 0, None
     if weight is not None:
-        if weight.dim() != 1 or weight.shape[0] != shape[-1] or not weight.is_contiguous() or weight.get_device() != dev:
+        if weight.shape != shape[-1:] or not weight.is_contiguous() or weight.get_device() != dev:
             raise ValueError("weight: contiguous [dim] of x's device")
         wt, wp = _type(weight, "weight"), weight.data_ptr()
     kind, os_, sp, ss = _out(out, out_scale, dev)
-    if x.numel() == 0:
+    if 0 in shape:
         return
     _call("qtea_rms_norm", dev, stream, x.data_ptr(), _type(x, "x"), xs, rp, rt, rs, wp, wt, eps, out.data_ptr(), kind, os_, sp, ss,
           shape[0], shape[1] if len(shape) == 3 else 1, shape[-1])
@@ -99,7 +101,7 @@ def qtea_silu_mul(gate, up, out, out_scale=None, stream=None):
         raise ValueError("gate, up and out: one shape [rows][dim], gate and up one type")
     gs, us = _tokens(gate, "gate", dev), _tokens(up, "up", dev)
     kind, os_, sp, ss = _out(out, out_scale, dev)
-    if gate.numel() == 0:
+    if 0 in gate.shape:
         return
     _call("qtea_silu_mul", dev, stream, gate.data_ptr(), up.data_ptr(), _type(gate, "gate and up"), gs, us, out.data_ptr(), kind, os_, sp, ss, *gate.shape)
 

@@ -163,6 +163,20 @@ def test_the_formats_range():
         assert np.array_equal(Y.double().cpu().numpy(), v @ W.T), x
 
 
+@pytest.mark.parametrize("byte", [10, 60, 127, 200, 246])
+def test_scales_of_the_activations(byte):
+    """The smallest and largest codes times the smallest and largest scales that are exact."""
+    W = np.zeros((2, 64))
+    W[0, 3], W[1, 33], W[1, 34] = 0.5, 1, -0.5
+    X = torch.zeros((3, 64), dtype=torch.uint8, device="cuda")
+    X[0, 3], X[1, 33], X[2, 33], X[2, 34] = 0x01, 0x7e, 0x81, 0xfe
+    xs = torch.full((3, 2), byte, dtype=torch.uint8, device="cuda")
+    Y = torch.empty((3, 2), device="cuda")
+    q.qtea_w4_gemm_lowbatch(q.pack_matrix_w4(_dev(W, "f32")), X, Y, x_scale=xs)
+    v = sv.decode(X.cpu().numpy(), xs.cpu().numpy(), "e4m3")
+    assert np.array_equal(Y.double().cpu().numpy(), (v @ W.T).astype(np.float32).astype(np.float64))
+
+
 @pytest.mark.parametrize("x", ["f16", "bf16", "e4m3"])
 def test_what_is_not_finite_stays_in_its_row(x):
     rng = np.random.default_rng(9)
