@@ -25,35 +25,33 @@ from paper_2609_00224_amd.serving import _TYPES, _call, _type
 _U8 = torch.uint8
 
 
-def _tokens(t, what, device):
-    """A dense operand, [tokens][dim] or [tokens][heads][dim] with a token's
-    part contiguous: the stride of its tokens (of one token it is not used,
-    whatever the view has)."""
-    shape, stride = t.shape, t.stride()
+def _tokens(t, run, what, device):
+    """A dense operand, [tokens][dim] or [tokens][heads][dim], whose tokens are
+    `run` elements, contiguous: the stride of its tokens (of one token it is not
+    used, whatever the view has)."""
     if t.get_device() != device:
         raise ValueError(f"{what}: a device tensor, a call's of one device")
-    n = len(shape)
-    if n == 2:
+    if t.is_contiguous():
+        return run
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 2:
         if stride[1] != 1 and shape[1] > 1:
             raise ValueError(f"{what}: a row's elements are contiguous")
-        return stride[0] if shape[0] > 1 else shape[1]
-    if n != 3:
-        raise ValueError(f"{what}: [rows][n] or [tokens][heads][n], got {list(shape)}")
-    if (stride[2] != 1 and shape[2] > 1) or (stride[1] != shape[2] and shape[1] > 1):
+    elif (stride[2] != 1 and shape[2] > 1) or (stride[1] != shape[2] and shape[1] > 1):
         raise ValueError(f"{what}: a token's heads and elements are contiguous")
-    return stride[0] if shape[0] > 1 else shape[1] * shape[2]
+    return stride[0] if shape[0] > 1 else run
 
 
-def _scales(codes, scale, what):
+def _scales(codes, scale, run, what):
     """The scale bytes of 8-bit rows: their address and row stride."""
-    if scale is None or scale.dtype is not _U8 or scale.dim() != codes.dim() or tuple(scale.shape) != (*codes.shape[:-1], codes.shape[-1] // 32):
+    if scale is None or scale.dtype is not _U8 or tuple(scale.shape) != (*codes.shape[:-1], codes.shape[-1] // 32):
         raise ValueError(f"{what}: uint8, one for each 32 codes of a row")
-    return scale.data_ptr(), _tokens(scale, what, codes.get_device())
+    return scale.data_ptr(), _tokens(scale, run // 32, what, codes.get_device())
 
 
-def _out(out, out_scale, device):
+def _out(out, out_scale, run, device):
     """An output's type, stride, scales and their stride."""
-    stride, kind = _tokens(out, "out", device), _TYPES.get(out.dtype)
+    stride, kind = _tokens(out, run, "out", device), _TYPES.get(out.dtype)
     if kind is not None:
         if out_scale is not None:
             raise ValueError("out_scale: for 8-bit outputs only")
@@ -62,7 +60,7 @@ def _out(out, out_scale, device):
         raise ValueError(f"out: fp16, bf16, fp32 or uint8 codes, got {out.dtype}")
     if out.shape[-1] % 32:
         raise ValueError("out: 8-bit rows are a multiple of 32 long")
-    return QTEA_E4M3, stride, *_scales(out, out_scale, "out_scale")
+    return QTEA_E4M3, stride, *_scales(out, out_scale, run, "out_scale")
 
 
 def qtea_rms_norm(x, weight, out, residual=None, eps: float = 1e-6, out_scale=None, stream=None):
@@ -74,20 +72,22 @@ def qtea_rms_norm(x, weight, out, residual=None, eps: float = 1e-6, out_scale=No
     shape, dev = x.shape, x.get_device()
     if dev < 0:
         raise ValueError("qtea entry points take device tensors")
-    if out.shape != shape or (residual is not None and residual.shape != shape):
-        raise ValueError("x, out and residual: one shape")
-    xs = _tokens(x, "x", dev)
-    rs, rt, rp = (0, 0, None) if residual is None else (_tokens(residual, "residual", dev), _type(residual, "residual"), residual.data_ptr())
+    heads = 1 if len(shape) == 2 else (shape[1] if len(shape) == 3 else 0)
+    if heads == 0 or out.shape != shape or (residual is not None and residual.shape != shape):
+        raise ValueError("x, out and residual: one shape, [rows][dim] or [tokens][heads][dim]")
+    run = heads * shape[-1]
+    xs = _tokens(x, run, "x", dev)
+    rs, rt, rp = (0, 0, None) if residual is None else (_tokens(residual, run, "residual", dev), _type(residual, "residual"), residual.data_ptr())
     wt, wp = 0, None
     if weight is not None:
         if weight.shape != shape[-1:] or not weight.is_contiguous() or weight.get_device() != dev:
             raise ValueError("weight: contiguous [dim] of x's device")
         wt, wp = _type(weight, "weight"), weight.data_ptr()
-    kind, os_, sp, ss = _out(out, out_scale, dev)
+    kind, os_, sp, ss = _out(out, out_scale, run, dev)
     if 0 in shape:
         return
     _call("qtea_rms_norm", dev, stream, x.data_ptr(), _type(x, "x"), xs, rp, rt, rs, wp, wt, eps, out.data_ptr(), kind, os_, sp, ss,
-          shape[0], shape[1] if len(shape) == 3 else 1, shape[-1])
+          shape[0], heads, shape[-1])
 
 
 def qtea_silu_mul(gate, up, out, out_scale=None, stream=None):
@@ -97,13 +97,15 @@ def qtea_silu_mul(gate, up, out, out_scale=None, stream=None):
     dev = gate.get_device()
     if dev < 0:
         raise ValueError("qtea entry points take device tensors")
-    if gate.dim() != 2 or up.shape != gate.shape or out.shape != gate.shape or up.dtype != gate.dtype:
+    shape = gate.shape
+    if len(shape) != 2 or up.shape != shape or out.shape != shape or up.dtype is not gate.dtype:
         raise ValueError("gate, up and out: one shape [rows][dim], gate and up one type")
-    gs, us = _tokens(gate, "gate", dev), _tokens(up, "up", dev)
-    kind, os_, sp, ss = _out(out, out_scale, dev)
-    if 0 in gate.shape:
+    rows, dim = shape
+    gs, us = _tokens(gate, dim, "gate", dev), _tokens(up, dim, "up", dev)
+    kind, os_, sp, ss = _out(out, out_scale, dim, dev)
+    if rows == 0 or dim == 0:
         return
-    _call("qtea_silu_mul", dev, stream, gate.data_ptr(), up.data_ptr(), _type(gate, "gate and up"), gs, us, out.data_ptr(), kind, os_, sp, ss, *gate.shape)
+    _call("qtea_silu_mul", dev, stream, gate.data_ptr(), up.data_ptr(), _type(gate, "gate and up"), gs, us, out.data_ptr(), kind, os_, sp, ss, rows, dim)
 
 
 # ---------------------------------------------------------------------------
@@ -158,19 +160,20 @@ def pack_matrix_w4(W, stream=None) -> W4Matrix:
 def qtea_w4_gemm_lowbatch(matrix: W4Matrix, X, Y, x_scale=None, stream=None):
     """Y = X W^T: X [rows][K] fp16 or bf16, or uint8 E4M3 codes with x_scale; Y
     [rows][N] fp16, bf16 or fp32; up to QTEA_W4_MAX_BATCH rows of any stride."""
-    packed, dev = matrix.packed, X.get_device()
-    if X.dim() != 2 or Y.dim() != 2 or X.shape[1] != matrix.K or Y.shape[1] != matrix.N or X.shape[0] != Y.shape[0]:
-        raise ValueError(f"X: [rows][{matrix.K}], Y: [rows][{matrix.N}]")
+    packed, dev, N, K = matrix.packed, X.get_device(), matrix.N, matrix.K
+    rows = X.shape[0]
+    if tuple(X.shape) != (rows, K) or tuple(Y.shape) != (rows, N):
+        raise ValueError(f"X: [rows][{K}], Y: [rows][{N}]")
     if dev < 0 or packed.get_device() != dev or not packed.is_contiguous():
         raise ValueError("X and the matrix: tensors of one device")
-    xs, ys = _tokens(X, "X", dev), _tokens(Y, "Y", dev)
+    xs, ys = _tokens(X, K, "X", dev), _tokens(Y, N, "Y", dev)
     if X.dtype is _U8:
-        kind, (sp, ss) = QTEA_E4M3, _scales(X, x_scale, "x_scale")
+        kind, (sp, ss) = QTEA_E4M3, _scales(X, x_scale, K, "x_scale")
     else:
         kind, sp, ss = _type(X, "X"), None, 0
         if x_scale is not None:
             raise ValueError("x_scale: for 8-bit rows only")
-    if X.shape[0] == 0:
+    if rows == 0:
         return
-    _call("qtea_w4_gemm_lowbatch", dev, stream, packed.data_ptr(), packed.numel() * packed.element_size(), matrix.N, matrix.K, X.data_ptr(), kind, xs,
-          sp, ss, X.shape[0], Y.data_ptr(), _type(Y, "Y"), ys)
+    _call("qtea_w4_gemm_lowbatch", dev, stream, packed.data_ptr(), packed.numel() * packed.element_size(), N, K, X.data_ptr(), kind, xs,
+          sp, ss, rows, Y.data_ptr(), _type(Y, "Y"), ys)

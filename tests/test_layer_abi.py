@@ -114,3 +114,13 @@ def test_oracle_by_hand():
     assert np.allclose(ol.rotate(x, [1], quarter), [[[-2, 1, 0, 3, 4, 5]]], atol=1e-6)
     assert np.allclose(ol.rotate(x, [1], quarter, True), [[[-1, 0, 2, 3, 4, 5]]], atol=1e-6)
     assert np.array_equal(ol.w4_values(np.array([[6.0, 0.3, -5.0]])), [[6, 0.5, -4]])  # a tie goes to the even code
+
+
+def test_the_binding_checks_shapes_before_devices_are_asked_for():
+    z = lambda *s, dt=torch.float32: torch.zeros(s, dtype=dt)  # noqa: E731
+    m = q.W4Matrix(3, 64, z(64, dt=torch.uint8))
+    for call in (lambda: q.qtea_w4_gemm_lowbatch(m, z(64), z(3)), lambda: q.qtea_w4_gemm_lowbatch(m, z(2, 1, 64), z(2, 1, 3)),
+                 lambda: q.qtea_w4_gemm_lowbatch(m, z(2, 64), z(3, 3)), lambda: q.qtea_rms_norm(z(64), None, z(64)),
+                 lambda: q.qtea_w4_unpack(m, z(3, 64))):
+        with pytest.raises(ValueError):
+            call()
