@@ -7,7 +7,8 @@
 //   scales  [ceil(K/512)][ceil(N/16)][64 lanes][4 bytes], byte i that of tile 4 u + i
 // Strips of 16 rows lie next to each other, so that what the waves of the chip
 // read at a time, a column of tiles, is one piece (against strip after strip:
-// 128257 x 4096 at 16 rows 50.0 us for 55.6, at one 49.4 for 53.0).
+// 128257 x 4096 at 16 rows 50.0 us for 55.6, at one 49.4 for 53.0, both with loads
+// that the caches keep).
 // Rows and columns past the matrix are zeros.
 #include <algorithm>
 #include <type_traits>
@@ -161,7 +162,11 @@ __device__ __forceinline__ uint64_t scalar(const uint8_t* p) {
   asm volatile("" : "+s"(at));
   return at;
 }
-__device__ __forceinline__ u32x4 load_codes(uint64_t p, uint32_t lane, int r) { return *reinterpret_cast<global_t<u32x4>*>(p + lane * 16 + r * kTile); }
+template <bool STREAM>
+__device__ __forceinline__ u32x4 load_codes(uint64_t p, uint32_t lane, int r) {
+  global_t<u32x4>* at = reinterpret_cast<global_t<u32x4>*>(p + lane * 16 + r * kTile);
+  return STREAM ? __builtin_nontemporal_load(at) : *at;
+}
 __device__ __forceinline__ uint32_t load_scale4(uint64_t p, uint32_t lane, int r) { return *reinterpret_cast<global_t<uint32_t>*>(p + lane * 4 + r * kUnitScales); }
 
 // A value that is computed where it is used instead of being held in
@@ -277,7 +282,7 @@ __global__ __launch_bounds__(kThreads) void w4_gemm_split_kernel(const GemmArgs 
     auto load = [&](int u, int j) {
       const uint64_t p = scalar(codes + int64_t(min(4 * u + j, a.tiles - 1)) * a.strips * kTile);
 #pragma unroll
-      for (int r = 0; r < R; ++r) w[j][r] = load_codes(p, lane, r);
+      for (int r = 0; r < R; ++r) w[j][r] = load_codes<false>(p, lane, r);
     };
     auto load_scales = [&](int u, uint32_t (&to)[R]) {
       const uint64_t p = scalar(scales + int64_t(u) * a.strips * kUnitScales);
@@ -359,10 +364,10 @@ __global__ __launch_bounds__(kThreads) void w4_gemm_split_kernel(const GemmArgs 
 // share their strips, each has a tile or two of every unit's four, and their
 // sums are added at the end: so a workgroup has four strips a wave to keep LDS
 // idle enough, and as few strips altogether as give every CU its share.  HBM bounds it
-// (128257 x 4096 at one row 49 us, 5.7 TB/s; a plain read of as many bytes 42), past 32
+// (128257 x 4096 at one row 45.5 us, 6.1 TB/s; a plain read of as many bytes 42), past 32
 // rows what a CU has to bring, decode and multiply (32000 x 5120 at 40 rows 24 us,
-// 16.6 at 16).
-template <int XT, int CT, int PARTS>
+// 17 at 16).  STREAM: codes are loaded as used once.
+template <int XT, int CT, int PARTS, bool STREAM>
 __global__ __launch_bounds__(kThreads) void w4_gemm_wide_kernel(const GemmArgs a) {
   using T = Type<XT>;
   constexpr int R = kWideStrips, TILES = 4 / PARTS;  // strips of a wave, tiles of a unit
@@ -381,7 +386,7 @@ __global__ __launch_bounds__(kThreads) void w4_gemm_wide_kernel(const GemmArgs a
   auto load = [&](int s, int u, int j) {
     const uint64_t p = scalar(codes + int64_t(min(4 * u + tile0 + j, a.tiles - 1)) * a.strips * kTile);  // (past the last tile: that one again, times zeros)
 #pragma unroll
-    for (int r = 0; r < R; ++r) w[s][j][r] = load_codes(p, lane, r);
+    for (int r = 0; r < R; ++r) w[s][j][r] = load_codes<STREAM>(p, lane, r);
   };
   auto load_scales = [&](int s, int u) {
     const uint64_t p = scalar(scales + int64_t(min(u, a.units - 1)) * a.strips * kUnitScales);
@@ -531,9 +536,9 @@ int compute_units() {
 
 using std::integral_constant;
 
-template <int XT, int CT, int PARTS>
+template <int XT, int CT, int PARTS, bool STREAM>
 int run_wide(const GemmArgs& a, hipStream_t st) {
-  const auto kernel = w4_gemm_wide_kernel<XT, CT, PARTS>;
+  const auto kernel = w4_gemm_wide_kernel<XT, CT, PARTS, STREAM>;
   static std::atomic<int> allowed[qtea_detail::kMaxDevices];
   constexpr int lds = 2 * 4 * CT * 4 * 64 * 16, strips = kWideStrips * kWaves / PARTS;
   if (qtea_detail::allow_lds(reinterpret_cast<const void*>(kernel), lds, allowed) != hipSuccess) return QTEA_ERR_HIP;
@@ -571,15 +576,25 @@ int run_gemm(GemmArgs a, int cus, hipStream_t st) {
       const int64_t blocks = (int64_t(a.strips) + n - 1) / n, most = (blocks + cus - 1) / cus * n;
       if (most < least && (n == 32 || blocks < (1 << 22))) least = most, strips = n;  // (a grid has 2^32 threads)
     }
-    const auto with = [&](auto cols) {
+    // A matrix of more than half of the Infinity Cache's 256 MB will not be there at the
+    // next call, and its codes are loaded as used once: 128257 x 4096 (279 MB) at one
+    // row 45.5 us for 49.9, 57344 x 8192 (250 MB) at 16 rows 43.2 for 46.3.  A smaller
+    // one may be kept: 28672 x 4096 (62 MB) at one row 13.4 for 12.7 where three take
+    // turns, though 13.5 for 13.9 where nine do.
+    const bool stream = int64_t(a.strips) * a.tiles * kTile > (128 << 20);
+    const auto with = [&](auto cols, auto past) {
       constexpr int CT = decltype(cols)::value;
-      if (strips == 32) return run_wide<XT, CT, 1>(a, st);
-      if (strips == 16) return run_wide<XT, CT, 2>(a, st);
-      return run_wide<XT, CT, 4>(a, st);
+      constexpr bool STREAM = decltype(past)::value;
+      if (strips == 32) return run_wide<XT, CT, 1, STREAM>(a, st);
+      if (strips == 16) return run_wide<XT, CT, 2, STREAM>(a, st);
+      return run_wide<XT, CT, 4, STREAM>(a, st);
     };
-    if (ct == 1) return with(integral_constant<int, 1>());
-    if (ct == 2) return with(integral_constant<int, 2>());
-    return ct == 3 ? with(integral_constant<int, 3>()) : with(integral_constant<int, 4>());
+    const auto by_cols = [&](auto past) {
+      if (ct == 1) return with(integral_constant<int, 1>(), past);
+      if (ct == 2) return with(integral_constant<int, 2>(), past);
+      return ct == 3 ? with(integral_constant<int, 3>(), past) : with(integral_constant<int, 4>(), past);
+    };
+    return stream ? by_cols(std::true_type()) : by_cols(std::false_type());
   }
   // Strips a group: the most that leave groups for six CUs of ten (10240 x 8192 at 16
   // rows 12.5 us with four, 16.2 with two; 8192 x 28672: 37.5 with four, that is
