@@ -72,6 +72,8 @@ int qtea_rms_norm(const void* x, int x_type, int64_t x_stride, void* residual, i
 
 /*
  * Gated activation: out = gate / (1 + exp(-gate)) * up, element by element.
+ * The factor 1 / (1 + exp(-gate)) is 0 where it is below 2^-126 (gates
+ * below -87).
  *
  *   gate, up   device [rows][dim] of `type` (enum qtea_type), gate_stride and
  *              up_stride elements from row to row (>= dim): the two halves of

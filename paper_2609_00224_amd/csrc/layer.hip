@@ -245,7 +245,7 @@ struct GateArgs {
 
 // g / (1 + exp(-g)) u.  exp(-g) = 2^t, t = -g log2(e): for results of 32 bits with what
 // the product's rounding left of t (it moves the power by up to 88 half ulps); the
-// others round to 2^-12 or more of themselves.
+// others round to 2^-12 or more of themselves.  (The reciprocal has no denormals.)
 template <bool FULL>
 __device__ __forceinline__ float gated(float g, float u) {
   constexpr float kLog2e = 0x1.715476p+0f, kRest = 0x1.4ae0cp-26f;  // log2(e) = kLog2e + kRest to 48 bits

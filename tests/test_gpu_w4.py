@@ -121,6 +121,15 @@ def test_many_rows_of_weights(N, K, batch, x):
     assert (room[batch:] == 7).all() and (room[:, N:] == 7).all()
 
 
+@pytest.mark.parametrize("x", ["f16", "bf16", "e4m3"])
+@pytest.mark.parametrize("batch", [1, 17, 33, 64])
+@pytest.mark.parametrize("N,K", [(57330, 4896), (65540, 4224), (128257, 2112)])
+def test_matrices_that_no_cache_keeps(N, K, batch, x):
+    """More than 128 MB of codes, 16, 8 and 32 strips a workgroup; exact sums."""
+    assert q.qtea_w4_packed_bytes(N, K) * 16 // 17 > 128 << 20
+    test_many_rows_of_weights(N, K, batch, x)
+
+
 @pytest.mark.parametrize("N", [90, 24000])
 @pytest.mark.parametrize("K,shift,pad", [(1000, 0, 8), (1000, 1, 0), (999, 0, 0), (1024, 3, 2), (4096, 0, 1), (130, 5, 6)])
 def test_rows_of_any_stride(K, shift, pad, N):
