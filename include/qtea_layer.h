@@ -71,9 +71,11 @@ int qtea_rms_norm(const void* x, int x_type, int64_t x_stride, void* residual, i
                   uint8_t* out_scale, int64_t scale_stride, int64_t tokens, int heads, int64_t dim, void* stream);
 
 /*
- * Gated activation: out = gate / (1 + exp(-gate)) * up, element by element.
- * The factor 1 / (1 + exp(-gate)) is 0 where it is below 2^-126 (gates
- * below -87).
+ * Gated activation: out = gate / (1 + exp(-gate)) * up, element by element, in
+ * fp32 before the rounding to out_type.  A factor below fp32's range (gates below
+ * -87) is as good as another; a gate that is itself below 2^-126 in magnitude is
+ * multiplied by its factor to fp32's smallest step, 2^-149.  A gate of -infinity
+ * gives NaN, as the formula does.
  *
  *   gate, up   device [rows][dim] of `type` (enum qtea_type), gate_stride and
  *              up_stride elements from row to row (>= dim): the two halves of

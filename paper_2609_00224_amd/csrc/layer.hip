@@ -244,11 +244,11 @@ struct GateArgs {
 };
 
 // g / (1 + exp(-g)) u.  exp(-g) = 2^t, t = -g log2(e): for results of 32 bits with what
-// the product's rounding left of t (it moves the power by up to 88 half ulps); the
-// others round to 2^-12 or more of themselves.  (The reciprocal has no denormals.)
+// the product's rounding left of t (it moves the power by up to 96 half ulps); the
+// others round to 2^-12 or more of themselves.
+constexpr float kLog2e = 0x1.715476p+0f, kRest = 0x1.4ae0cp-26f;  // log2(e) = kLog2e + kRest to 48 bits
 template <bool FULL>
 __device__ __forceinline__ float gated(float g, float u) {
-  constexpr float kLog2e = 0x1.715476p+0f, kRest = 0x1.4ae0cp-26f;  // log2(e) = kLog2e + kRest to 48 bits
   const float t = -g * kLog2e;
   float e = __builtin_amdgcn_exp2f(t);
   if constexpr (FULL) {
@@ -257,6 +257,34 @@ __device__ __forceinline__ float gated(float g, float u) {
     e = __builtin_fabsf(t) < 126.0f ? better : e;
   }
   return g * __builtin_amdgcn_rcpf(1.0f + e) * u;
+}
+
+// The same below kLow, where the factor leaves the numbers of 32 bits while a large u
+// keeps the result among them (and the reciprocal, which has no denormals, gives 0
+// for 1 + e from 2^126 on): 1 + e is e there, g 2^n 2^f with n + f = -t, the power taken
+// in two steps with u between them.  A gate below -512 is taken as -512: times the
+// largest u that is 2^-601, which is 0 as well.
+constexpr float kLow = -80.0f;
+__device__ float gated_low(float g, float u) {
+  g = fmaxf(g, -512.0f);
+  const float n = __builtin_rintf(g * kLog2e), f = __builtin_fmaf(g, kRest, __builtin_fmaf(g, kLog2e, -n));
+  const float y = __builtin_amdgcn_ldexpf(g * __builtin_amdgcn_exp2f(f), -60) * u;
+  return __builtin_amdgcn_ldexpf(y, int(n) + 60);
+}
+
+// 8 of them, into g.  (-infinity stays the formula's NaN.)
+template <bool FULL>
+__device__ __forceinline__ void gated8(float (&g)[8], const float (&u)[8]) {
+  float y[8], least = g[0];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) y[k] = gated<FULL>(g[k], u[k]), least = fminf(least, g[k]);
+  if (least < kLow) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (g[k] < kLow && g[k] >= -0x1.fffffep127f) y[k] = gated_low(g[k], u[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) g[k] = y[k];
 }
 
 template <int T, int OT, int OCTS>
@@ -277,8 +305,7 @@ __global__ __launch_bounds__(kThreads) void silu_mul_kernel(const GateArgs a) {
       float g[8], u[8];
       values<T>(rg[i], g);
       values<T>(ru[i], u);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) g[k] = gated<OT == QTEA_F32>(g[k], u[k]);
+      gated8<OT == QTEA_F32>(g, u);
       store_oct<OT>(a.out, row[i], at[i], g);
     }
   }
@@ -292,8 +319,7 @@ __global__ __launch_bounds__(kThreads) void silu_mul_any_kernel(const GateArgs a
     float g[8], u[8];
     load_any(a.type, a.gate + int64_t(row) * a.gate_stride, at, n, a.gate_wide, g);
     load_any(a.type, a.up + int64_t(row) * a.up_stride, at, n, a.up_wide, u);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) g[i] = gated<true>(g[i], u[i]);
+    gated8<true>(g, u);
     store_out(a.out, row, at, n, g);
   }
 }

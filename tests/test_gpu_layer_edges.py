@@ -1,0 +1,57 @@
+"""The layer operators where their ranges end: small results, alignments, sizes
+past 2^29, paths that only large or odd operands take."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+import oracle.layer as ol
+import paper_2609_00224_amd as q
+from tests.layer_cases import TORCH, U, check, room, rounded
+
+pytestmark = pytest.mark.gpu
+
+
+# -- the gated activation -----------------------------------------------------------
+def _gate_error(gate, want, out):
+    """What fp32 may be off before the last rounding: an exp2 and a reciprocal of an
+    ulp (two half ulps) each, the sum and three products half an ulp each.  Results
+    that are not fp32 may carry the exponent's rounding too: t = -g log2(e) is off by
+    half an ulp and by the constant's 2^-26, 1.2 |t| U, which moves exp(-g) by that times
+    ln 2, and the result by no more of itself."""
+    return U * np.abs(want) * (8 + (0 if out == "f32" else 1.25 * np.abs(gate)))
+
+
+@pytest.mark.parametrize("x,out", [("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16"), ("bf16", "f32"), ("bf16", "e4m3")])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_gate_where_the_factor_leaves_32_bits(x, out, shift):
+    """Gates of -75 to -260 times values up to the type's largest: the factor is
+    below 2^-126 from -87.3 on, the result a normal number far beyond that."""
+    rng = np.random.default_rng([len(x), len(out), shift])
+    rows, dim = 7, 992
+    gate = rounded(-rng.uniform(75, 260, (rows, dim)), x)
+    up = rounded(rng.choice([-1, 1], (rows, dim)) * rng.uniform(1, 1.9, (rows, dim)) * 2.0 ** rng.integers(-10, 128, (rows, dim)), x)
+    gate[:, 0::32], up[:, 0::32] = rounded(np.float64(-88), x), 1000
+    wide = torch.zeros((rows, 2 * dim + shift), dtype=TORCH[x], device="cuda")
+    wide[:, shift:] = torch.from_numpy(np.concatenate((gate, up), 1)).to(TORCH[x])
+    got, scale = room((rows, dim), out)
+    q.qtea_silu_mul(wide[:, shift:shift + dim], wide[:, shift + dim:], got, out_scale=scale)
+    want = ol.silu_mul(gate, up)
+    assert (np.abs(want) >= 2.0 ** -126).mean() > 0.2
+    # (the last product in 32 bits may be rounded to its smallest step)
+    check(got, scale, want, out, _gate_error(gate, want, out) + 2.0 ** -150)
+
+
+def test_gate_far_below_and_not_finite():
+    """Whatever a gate below -512 meets: 0 times finite values, the formula's
+    infinity or NaN times the others."""
+    inf, nan = float("inf"), float("nan")
+    g = torch.tensor([[-513.0, -1e4, -3e38, -100.0, -1e4, -3e38, -100.0, -3e38, -inf, -inf, -600.0, nan, -90.0, -90.0, -81.0, -81.0]], device="cuda")
+    u = torch.tensor([[3e38, -3e38, 3e38, inf, -inf, inf, nan, nan, 0.0, 1.0, 0.0, 1e30, 0.0, -0.0, inf, -1.0]], device="cuda")
+    out = torch.empty_like(g)
+    q.qtea_silu_mul(g, u, out)
+    got = out[0].tolist()
+    assert got[:3] == [0, 0, 0] and got[3] == -inf and got[4] == inf and got[5] == -inf and got[10] == 0 and got[12] == got[13] == 0 and got[14] == -inf
+    assert out[0, [6, 7, 8, 9, 11]].isnan().all()
+    assert abs(got[15] - 81 * np.exp(-81.0)) <= 8 * U * 81 * np.exp(-81.0)
