@@ -319,7 +319,9 @@ __global__ __launch_bounds__(kThreads) void silu_mul_any_kernel(const GateArgs a
     float g[8], u[8];
     load_any(a.type, a.gate + int64_t(row) * a.gate_stride, at, n, a.gate_wide, g);
     load_any(a.type, a.up + int64_t(row) * a.up_stride, at, n, a.up_wide, u);
-    gated8<true>(g, u);
+    // (the aligned kernel's arithmetic for each type of result)
+    if (a.out.type == QTEA_F32) gated8<true>(g, u);
+    else gated8<false>(g, u);
     store_out(a.out, row, at, n, g);
   }
 }

@@ -55,3 +55,23 @@ def test_gate_far_below_and_not_finite():
     assert got[:3] == [0, 0, 0] and got[3] == -inf and got[4] == inf and got[5] == -inf and got[10] == 0 and got[12] == got[13] == 0 and got[14] == -inf
     assert out[0, [6, 7, 8, 9, 11]].isnan().all()
     assert abs(got[15] - 81 * np.exp(-81.0)) <= 8 * U * 81 * np.exp(-81.0)
+
+
+@pytest.mark.parametrize("out", ["f16", "bf16", "f32", "e4m3"])
+@pytest.mark.parametrize("x", ["f16", "bf16", "f32"])
+def test_gate_has_the_same_bits_at_any_alignment(x, out):
+    """Aligned rows, shifted inputs and a shifted output take different kernels."""
+    rng = np.random.default_rng([len(x), len(out)])
+    rows, dim = 40, 4096
+    both = torch.from_numpy(rng.standard_normal((rows, 2 * dim)) * rng.choice([1, 10, 40], (rows, 2 * dim))).to(TORCH[x]).cuda()
+    want, want_scale = room((rows, dim), out)
+    q.qtea_silu_mul(both[:, :dim], both[:, dim:], want, out_scale=want_scale)
+    wide = torch.zeros((rows, 2 * dim + 1), dtype=TORCH[x], device="cuda")
+    wide[:, 1:] = both
+    got, scale = room((rows, dim), out)
+    q.qtea_silu_mul(wide[:, 1:1 + dim], wide[:, 1 + dim:], got, out_scale=scale)
+    assert torch.equal(got, want) and (scale is None or torch.equal(scale, want_scale))
+    if out != "e4m3":
+        got = torch.zeros((rows, dim + 1), dtype=TORCH[out], device="cuda")[:, 1:]
+        q.qtea_silu_mul(both[:, :dim], both[:, dim:], got)
+        assert torch.equal(got, want)
