@@ -36,6 +36,11 @@ enum { QTEA_E4M3 = 3 }; /* beside enum qtea_type */
 
 #define QTEA_NORM_MAX_DIM 65536 /* longest row of qtea_rms_norm */
 #define QTEA_W4_MAX_BATCH 64    /* most rows of one qtea_w4_gemm_lowbatch */
+/*
+ * Strides are at most QTEA_MAX_STRIDE elements, and one times the rows that
+ * it separates at most 2^60.
+ */
+#define QTEA_MAX_STRIDE (INT64_C(1) << 38)
 
 /*
  * Root-mean-square norm of rows of dim values, with the residual's addition:
@@ -61,6 +66,8 @@ enum { QTEA_E4M3 = 3 }; /* beside enum qtea_type */
  *              out_stride a multiple of 16
  *   out_scale  device uint8 [tokens][heads * dim / 32], scale_stride bytes
  *              from token to token (QTEA_E4M3; NULL otherwise)
+ *   tokens     up to 2^31 - 1
+ *   heads      1 .. 65535
  *   dim        1 .. QTEA_NORM_MAX_DIM
  * Operands are aligned to their elements; rows that are 16-byte aligned move
  * in wide accesses.  Sums are fp32: |t| up to about 1e18.
@@ -82,7 +89,7 @@ int qtea_rms_norm(const void* x, int x_type, int64_t x_stride, void* residual, i
  *              one product's output can be passed in place
  *   out, out_scale  as qtea_rms_norm's; out may be gate or up itself (same
  *              type, same stride)
- *   rows * ceil(dim / 8) below 2^31
+ *   rows, dim  up to 2^31 - 1, rows * ceil(dim / 8) below 2^31
  * Errors: QTEA_ERR_INVALID_ARG, QTEA_ERR_HIP.
  */
 int qtea_silu_mul(const void* gate, const void* up, int type, int64_t gate_stride, int64_t up_stride, void* out,

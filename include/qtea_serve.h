@@ -105,7 +105,7 @@ typedef struct qtea_kv_batch {
  *             qtea_type), `k_stride` / `v_stride` elements from one token
  *             to the next (>= n_heads * head_dim): columns of a fused
  *             projection's output can be passed in place.  16-byte aligned,
- *             strides a multiple of 16 bytes.
+ *             strides a multiple of 16 bytes, below 2^29 elements.
  * 16-bit formats: rounded to nearest.  Quantized formats, per block of 32
  * channels: the scale is the smallest power of two 2^e with
  * max|x| <= 448 * 2^e, -15 <= e <= 7 (E4M3) or max|x| <= 6 * 2^e,

@@ -366,7 +366,7 @@ int qtea_kv_append_rotated(const qtea_kv_cache* cache, const qtea_kv_batch* batc
   if (rot_dim < 16 || rot_dim > cache->head_dim || rot_dim % 16 != 0 || q_out_type < QTEA_F16 || q_out_type > QTEA_F32) return QTEA_ERR_INVALID_ARG;
   if (n_q_heads > 0) {
     const int64_t width = int64_t(n_q_heads) * cache->head_dim;
-    if (!q || !q_out || !stride_ok(q_stride, width) || !stride_ok(q_out_stride, width)) return QTEA_ERR_INVALID_ARG;
+    if (!q || !q_out || !stride_ok(q_stride, width, batch->n_tokens) || !stride_ok(q_out_stride, width, batch->n_tokens)) return QTEA_ERR_INVALID_ARG;
     if (!rows_aligned16(q, q_stride, type) || !rows_aligned16(q_out, q_out_stride, q_out_type)) return QTEA_ERR_INVALID_ARG;
     if (q == q_out && (type != q_out_type || q_stride != q_out_stride)) return QTEA_ERR_INVALID_ARG;
   } else {

@@ -331,11 +331,11 @@ using std::integral_constant;
 
 bool dense_type(int type) { return type >= QTEA_F16 && type <= QTEA_F32; }
 
-// The host's checks of an output of `run` values a token; false if not valid.
-bool make_out(void* out, int type, int64_t stride, uint8_t* scale, int64_t scale_stride, int64_t run, int64_t dim, Out* o) {
-  if (!out || !stride_ok(stride, run)) return false;
+// The host's checks of an output of `rows` tokens of `run` values; false if not valid.
+bool make_out(void* out, int type, int64_t stride, uint8_t* scale, int64_t scale_stride, int64_t run, int64_t dim, int64_t rows, Out* o) {
+  if (!out || !stride_ok(stride, run, rows)) return false;
   if (type == QTEA_E4M3) {
-    if (dim % 32 != 0 || !rows_aligned16(out, stride, type) || !scale || !stride_ok(scale_stride, run / 32)) return false;
+    if (dim % 32 != 0 || !rows_aligned16(out, stride, type) || !scale || !stride_ok(scale_stride, run / 32, rows)) return false;
   } else if (!dense_type(type) || scale || !aligned_to_elem(out, type)) {
     return false;
   }
@@ -396,13 +396,13 @@ int qtea_rms_norm(const void* x, int x_type, int64_t x_stride, void* residual, i
                   uint8_t* out_scale, int64_t scale_stride, int64_t tokens, int heads, int64_t dim, void* stream) {
   if (!x || !dense_type(x_type) || tokens < 0 || tokens > INT32_MAX || heads < 1 || heads > 65535 || dim < 1 || dim > QTEA_NORM_MAX_DIM) return QTEA_ERR_INVALID_ARG;
   const int64_t run = heads * dim;
-  if (!stride_ok(x_stride, run) || !aligned_to_elem(x, x_type) || !(eps >= 0x1p-126f && eps <= 0x1.fffffep127f)) return QTEA_ERR_INVALID_ARG;
-  if (residual && (!dense_type(residual_type) || !stride_ok(residual_stride, run) || !aligned_to_elem(residual, residual_type))) return QTEA_ERR_INVALID_ARG;
+  if (!stride_ok(x_stride, run, tokens) || !aligned_to_elem(x, x_type) || !(eps >= 0x1p-126f && eps <= 0x1.fffffep127f)) return QTEA_ERR_INVALID_ARG;
+  if (residual && (!dense_type(residual_type) || !stride_ok(residual_stride, run, tokens) || !aligned_to_elem(residual, residual_type))) return QTEA_ERR_INVALID_ARG;
   if (residual && (residual == x || residual == out)) return QTEA_ERR_INVALID_ARG;
   if (weight && (!dense_type(weight_type) || !aligned_to_elem(weight, weight_type) || weight == out)) return QTEA_ERR_INVALID_ARG;
   if (x == out && (x_type != out_type || x_stride != out_stride)) return QTEA_ERR_INVALID_ARG;
   NormArgs a;
-  if (!make_out(out, out_type, out_stride, out_scale, scale_stride, run, dim, &a.out)) return QTEA_ERR_INVALID_ARG;
+  if (!make_out(out, out_type, out_stride, out_scale, scale_stride, run, dim, tokens, &a.out)) return QTEA_ERR_INVALID_ARG;
   if (tokens == 0) return QTEA_OK;
   a.x = static_cast<const char*>(x), a.residual = static_cast<char*>(residual), a.weight = static_cast<const char*>(weight);
   a.x_stride = x_stride * elem_bytes(x_type), a.residual_stride = residual ? residual_stride * elem_bytes(residual_type) : 0;
@@ -430,13 +430,13 @@ int qtea_silu_mul(const void* gate, const void* up, int type, int64_t gate_strid
                   int out_type, int64_t out_stride, uint8_t* out_scale, int64_t scale_stride, int64_t rows, int64_t dim,
                   void* stream) {
   if (!gate || !up || !dense_type(type) || rows < 0 || rows > INT32_MAX || dim < 1 || dim > INT32_MAX) return QTEA_ERR_INVALID_ARG;
-  if (!stride_ok(gate_stride, dim) || !stride_ok(up_stride, dim) || !aligned_to_elem(gate, type) || !aligned_to_elem(up, type)) return QTEA_ERR_INVALID_ARG;
+  if (!stride_ok(gate_stride, dim, rows) || !stride_ok(up_stride, dim, rows) || !aligned_to_elem(gate, type) || !aligned_to_elem(up, type)) return QTEA_ERR_INVALID_ARG;
   if (out == gate && (out_type != type || out_stride != gate_stride)) return QTEA_ERR_INVALID_ARG;
   if (out == up && (out_type != type || out_stride != up_stride)) return QTEA_ERR_INVALID_ARG;
   const int64_t octs = (dim + 7) / 8;
   if (rows * octs > INT32_MAX) return QTEA_ERR_INVALID_ARG;
   GateArgs a;
-  if (!make_out(out, out_type, out_stride, out_scale, scale_stride, dim, dim, &a.out)) return QTEA_ERR_INVALID_ARG;
+  if (!make_out(out, out_type, out_stride, out_scale, scale_stride, dim, dim, rows, &a.out)) return QTEA_ERR_INVALID_ARG;
   if (rows == 0) return QTEA_OK;
   a.gate = static_cast<const char*>(gate), a.up = static_cast<const char*>(up);
   a.gate_stride = gate_stride * elem_bytes(type), a.up_stride = up_stride * elem_bytes(type);

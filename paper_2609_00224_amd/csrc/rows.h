@@ -164,8 +164,11 @@ __device__ __forceinline__ u32x2 block_codes(float (&x)[8], uint32_t e) {
 // Host: whether rows `stride` elements apart from `p` are each 16-byte aligned.
 inline bool rows_aligned16(const void* p, int64_t stride, int type) { return aligned16(p) && stride * elem_bytes(type) % 16 == 0; }
 inline bool aligned_to_elem(const void* p, int type) { return reinterpret_cast<uintptr_t>(p) % elem_bytes(type) == 0; }
-// Host: strides whose byte offsets over 2^31 rows stay far inside 64 bits.
-inline bool stride_ok(int64_t stride, int64_t width) { return stride >= width && stride <= (INT64_MAX >> 34); }
+// Host: strides whose byte offsets over the call's rows stay far inside 64 bits
+// (QTEA_MAX_STRIDE is more than a card's memory holds).
+inline bool stride_ok(int64_t stride, int64_t width, int64_t rows) {
+  return stride >= width && stride <= QTEA_MAX_STRIDE && (rows <= 1 || stride <= (int64_t(1) << 60) / rows);
+}
 
 }  // namespace qtea_serve
 

@@ -509,7 +509,7 @@ namespace {
 
 bool pack_args(const void* packed, int64_t N, int64_t K, const void* W, int type, int64_t w_stride, Layout* l, PackArgs* a) {
   if (!packed || !W || !aligned16(packed) || type < QTEA_F16 || type > QTEA_F32 || !make_layout(N, K, l)) return false;
-  if (!stride_ok(w_stride, K) || !aligned_to_elem(W, type)) return false;
+  if (!stride_ok(w_stride, K, N) || !aligned_to_elem(W, type)) return false;
   a->w = static_cast<char*>(const_cast<void*>(W));
   a->codes = static_cast<uint8_t*>(const_cast<void*>(packed)), a->scales = a->codes + l->scales_at;
   a->stride = w_stride * elem_bytes(type), a->strips = l->strips, a->tiles = l->tiles, a->units = l->units, a->total = l->strips * l->units * 256;
@@ -658,9 +658,9 @@ int qtea_w4_gemm_lowbatch(const void* packed, int64_t packed_bytes, int64_t N, i
   Layout l;
   if (!packed || !X || !Y || !aligned16(packed) || !make_layout(N, K, &l)) return QTEA_ERR_INVALID_ARG;
   if (batch < 1 || batch > QTEA_W4_MAX_BATCH) return QTEA_ERR_BATCH;
-  if (y_type < QTEA_F16 || y_type > QTEA_F32 || !aligned_to_elem(Y, y_type) || !stride_ok(y_stride, N) || !stride_ok(x_stride, K)) return QTEA_ERR_INVALID_ARG;
+  if (y_type < QTEA_F16 || y_type > QTEA_F32 || !aligned_to_elem(Y, y_type) || !stride_ok(y_stride, N, batch) || !stride_ok(x_stride, K, batch)) return QTEA_ERR_INVALID_ARG;
   if (x_type == QTEA_E4M3) {
-    if (K % 32 != 0 || !rows_aligned16(X, x_stride, x_type) || !x_scale || !stride_ok(x_scale_stride, K / 32)) return QTEA_ERR_INVALID_ARG;
+    if (K % 32 != 0 || !rows_aligned16(X, x_stride, x_type) || !x_scale || !stride_ok(x_scale_stride, K / 32, batch)) return QTEA_ERR_INVALID_ARG;
   } else if ((x_type != QTEA_F16 && x_type != QTEA_BF16) || x_scale || !aligned_to_elem(X, x_type)) {
     return QTEA_ERR_INVALID_ARG;
   }

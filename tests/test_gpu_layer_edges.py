@@ -75,3 +75,51 @@ def test_gate_has_the_same_bits_at_any_alignment(x, out):
         got = torch.zeros((rows, dim + 1), dtype=TORCH[out], device="cuda")[:, 1:]
         q.qtea_silu_mul(both[:, :dim], both[:, dim:], got)
         assert torch.equal(got, want)
+
+
+# -- sizes past 2^29 ---------------------------------------------------------------------
+def test_gate_of_a_row_past_2_to_the_29():
+    dim = 2 ** 29 + 40
+    both = torch.empty((1, 2 * dim), dtype=torch.float16, device="cuda")
+    both[:, :dim], both[:, dim:] = 1.0, 2.0
+    both[0, dim - 1], both[0, -1], both[0, 5] = -2.0, 3.0, 0.0
+    out = torch.empty((1, dim), dtype=torch.float16, device="cuda")
+    q.qtea_silu_mul(both[:, :dim], both[:, dim:], out)
+    one = torch.tensor(2 / (1 + np.exp(-1.0))).half().item()
+    assert out[0, 5] == 0 and (out[0, 6:-1] == one).all() and abs(out[0, -1].item() + 6 / (1 + np.exp(2.0))) < 1e-3
+
+
+def test_norm_of_a_token_past_2_to_the_29():
+    heads, dim = 65535, 8224
+    assert heads * dim > 2 ** 29
+    x = torch.ones((2, heads, dim), dtype=torch.float16, device="cuda")
+    x[1, -1] = 4.0
+    x[1, -1, ::2] = -2.0
+    q.qtea_rms_norm(x, None, x, eps=1e-6)
+    want = torch.tensor([-2.0, 4.0]).div(10 ** 0.5).half().cuda()
+    assert (x[0] == 1).all() and (x[1, :-1] == 1).all() and torch.equal(x[1, -1, :2], want) and torch.equal(x[1, -1, -2:], want)
+
+
+@pytest.mark.parametrize("batch,offset", [(1, 0), (3, 0), (2, 1)])
+def test_product_of_more_than_2_to_the_29_rows(batch, offset):
+    """The packed matrix of up to 128 columns has one tile a strip, strip after strip, then
+    their scales: zeros, with the first and the last strips' from a small one."""
+    N, K = 2 ** 29 + 19, 40
+    strips = -(-N // 16)
+    m = q.W4Matrix(N, K, torch.zeros(q.qtea_w4_packed_bytes(N, K), dtype=torch.uint8, device="cuda"))
+    assert m.packed.numel() == strips * 1280
+    small = torch.zeros((32, K), device="cuda")
+    small[0, 3], small[16 + (N - 1) % 16, K - 1], small[16, 0] = 3.0, 1.5, -2.0
+    packed = q.pack_matrix_w4(small).packed
+    m.packed[strips * 1024:] = packed[2048 + 8]  # (a scale byte of zeros)
+    for at, strip in ((0, 0), (1, strips - 1)):
+        m.packed[strip * 1024:(strip + 1) * 1024] = packed[at * 1024:(at + 1) * 1024]
+        m.packed[strips * 1024 + strip * 256:strips * 1024 + (strip + 1) * 256] = packed[2048 + at * 256:2048 + (at + 1) * 256]
+    X = torch.zeros((batch, K + 2 * offset), dtype=torch.float16, device="cuda")[:, offset:offset + K]
+    X[:] = torch.arange(1, batch + 1, device="cuda")[:, None].half()
+    Y = torch.full((batch, N), 7.0, dtype=torch.float16, device="cuda")
+    q.qtea_w4_gemm_lowbatch(m, X, Y)
+    for b in range(batch):
+        y = Y[b]
+        assert y[0] == 3 * (b + 1) and y[-1] == 1.5 * (b + 1) and y[(strips - 1) * 16] == -2 * (b + 1)
+        assert int((y != 0).sum()) == 3
