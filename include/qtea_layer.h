@@ -36,6 +36,7 @@ enum { QTEA_E4M3 = 3 }; /* beside enum qtea_type */
 
 #define QTEA_NORM_MAX_DIM 65536 /* longest row of qtea_rms_norm */
 #define QTEA_W4_MAX_BATCH 64    /* most rows of one qtea_w4_gemm_lowbatch */
+#define QTEA_W4_MAX_ROWS 0x7fffff00 /* most rows of a matrix: 2^31 - 256 */
 /*
  * Strides are at most QTEA_MAX_STRIDE elements, and one times the rows that
  * it separates at most 2^60.
@@ -102,7 +103,7 @@ int qtea_silu_mul(const void* gate, const void* up, int type, int64_t gate_strid
  * qtea_kv_append's rule for E2M1: 4.25 bits per weight.  Every value of such a
  * block is an fp16 (and a bf16) value, and packing such values again gives
  * the same ones.  A block with a NaN or an infinity is NaN.
- * The packed buffer is opaque; N is 1 .. 2^31 - 1, K 1 .. 2^24.
+ * The packed buffer is opaque; N is 1 .. QTEA_W4_MAX_ROWS, K 1 .. 2^24.
  */
 int qtea_w4_packed_bytes(int64_t N, int64_t K, int64_t* out_bytes);
 

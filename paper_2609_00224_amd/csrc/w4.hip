@@ -27,7 +27,7 @@ struct Layout {
   int64_t strips, tiles, units, scales_at, bytes;  // of 16 rows; tiles and units of four tiles of a strip
 };
 bool make_layout(int64_t N, int64_t K, Layout* l) {
-  if (N < 1 || K < 1 || N > INT32_MAX || K > (1 << 24)) return false;
+  if (N < 1 || K < 1 || N > QTEA_W4_MAX_ROWS || K > (1 << 24)) return false;
   l->strips = (N + 15) / 16, l->tiles = (K + 127) / 128, l->units = (l->tiles + 3) / 4;
   l->scales_at = l->strips * l->tiles * kTile;
   l->bytes = l->scales_at + l->strips * l->units * kUnitScales;

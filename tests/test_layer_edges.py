@@ -27,7 +27,9 @@ def test_sizes_that_the_header_allows_are_not_refused():
 
 
 def test_sizes_that_no_grid_or_address_has_are_refused():
-    lib = q.load()
+    lib, out = q.load(), ctypes.c_int64(0)
+    for N in (2 ** 31 - 255, 2 ** 31 - 1):
+        assert lib.qtea_w4_packed_bytes(N, 1, ctypes.byref(out)) == q.QTEA_ERR_INVALID_ARG
     for tokens, stride in ((3, 2 ** 38 + 16), (2 ** 31 - 1, 2 ** 29 + 16), (1, 2 ** 62)):
         assert lib.qtea_rms_norm(ADDR, 1, stride, None, 0, 0, None, 0, 1e-6, OTHER, 1, 64, None, 0, tokens, 1, 64, None) == q.QTEA_ERR_INVALID_ARG
         assert lib.qtea_rms_norm(ADDR, 1, 64, None, 0, 0, None, 0, 1e-6, OTHER, 1, stride, None, 0, tokens, 1, 64, None) == q.QTEA_ERR_INVALID_ARG
