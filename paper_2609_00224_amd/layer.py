@@ -20,7 +20,7 @@ import torch
 
 import paper_2609_00224_amd as _q
 from paper_2609_00224_amd import QTEA_E4M3
-from paper_2609_00224_amd.serving import _TYPES, _call, _type
+from paper_2609_00224_amd.serving import _TYPES, _call, _int, _type
 
 _U8 = torch.uint8
 
@@ -87,7 +87,7 @@ def qtea_rms_norm(x, weight, out, residual=None, eps: float = 1e-6, out_scale=No
     if 0 in shape:
         return
     _call("qtea_rms_norm", dev, stream, x.data_ptr(), _type(x, "x"), xs, rp, rt, rs, wp, wt, eps, out.data_ptr(), kind, os_, sp, ss,
-          shape[0], heads, shape[-1])
+          shape[0], _int(heads), shape[-1])
 
 
 def qtea_silu_mul(gate, up, out, out_scale=None, stream=None):
@@ -176,4 +176,4 @@ def qtea_w4_gemm_lowbatch(matrix: W4Matrix, X, Y, x_scale=None, stream=None):
     if rows == 0:
         return
     _call("qtea_w4_gemm_lowbatch", dev, stream, packed.data_ptr(), packed.numel() * packed.element_size(), N, K, X.data_ptr(), kind, xs,
-          sp, ss, rows, Y.data_ptr(), _type(Y, "Y"), ys)
+          sp, ss, _int(rows), Y.data_ptr(), _type(Y, "Y"), ys)

@@ -23,6 +23,12 @@ _TYPES = {torch.float16: QTEA_F16, torch.bfloat16: QTEA_BF16, torch.float32: QTE
 _I32, _F32 = torch.int32, torch.float32
 
 
+def _int(n):
+    """A count as the C int that it is passed as: past its range the largest one,
+    which the entry points refuse."""
+    return min(n, 0x7fffffff)
+
+
 def _type(t, what):
     got = _TYPES.get(t.dtype)
     if got is None:
@@ -161,7 +167,7 @@ def qtea_kv_append_rotated(cache: KvCache, Q, k, v, q_start, kv_len, page_table,
     if n == 0:
         return
     _call("qtea_kv_append_rotated", cache.device_index, stream, cache.desc, b, None if Q is None else Q.data_ptr(), k.data_ptr(), v.data_ptr(),
-          _type(k, "k and v"), qs, ks, vs, heads, freq.data_ptr(), 2 * freq.numel(), bool(interleaved), None if Q is None else q_out.data_ptr(), kind, os_)
+          _type(k, "k and v"), qs, ks, vs, _int(heads), freq.data_ptr(), _int(2 * freq.numel()), bool(interleaved), None if Q is None else q_out.data_ptr(), kind, os_)
 
 
 def qtea_kv_read(cache: KvCache, q_start, kv_len, page_table, k, v, stream=None):
