@@ -126,8 +126,9 @@ int qtea_kv_append(const qtea_kv_cache* cache, const qtea_kv_batch* batch, const
  *   (a, b) <- (a cos - b sin, b cos + a sin),
  *
  * pair i being channels i and i + rot_dim / 2, or, interleaved, 2i and 2i + 1.
- * The angle is taken in 64 bits, its sine and cosine and the products in 32;
- * then one rounding, to q_out_type or the cache's format.
+ * The angle, its sine and its cosine are taken in 64 bits (off by at most 2^-36 at
+ * angles up to 2^46, 2^-28 up to 2^51) and rounded to 32, the products are taken
+ * in 32; then one rounding, to q_out_type or the cache's format.
  *
  *   q, k, v     device [n_tokens][n_q_heads (q) or n_heads][head_dim] of
  *               `type`, strides and alignment as qtea_kv_append's: the three

@@ -123,3 +123,42 @@ def test_product_of_more_than_2_to_the_29_rows(batch, offset):
         y = Y[b]
         assert y[0] == 3 * (b + 1) and y[-1] == 1.5 * (b + 1) and y[(strips - 1) * 16] == -2 * (b + 1)
         assert int((y != 0).sum()) == 3
+
+
+# -- the rotation ------------------------------------------------------------------------
+def _turn_error(x, pos, freq, interleaved):
+    """Sine and cosine are found in 64 bits, to a tenth of half an ulp of fp32 at any angle
+    (and 2^-50 next to their zeros), and rounded once; the two products are rounded
+    once each.  So |a cos| and |b sin| are off by 2.1 U of themselves; their sum's
+    rounding is the result's."""
+    half = len(freq)
+    angle = np.asarray(pos, np.longdouble)[:, None] * np.asarray(freq, np.longdouble)
+    cos, sin = np.abs(np.cos(angle)).astype(np.float64)[:, None], np.abs(np.sin(angle)).astype(np.float64)[:, None]
+    a, b = (np.arange(half) * 2, np.arange(half) * 2 + 1) if interleaved else (np.arange(half), np.arange(half) + half)
+    x, err = np.abs(x), np.zeros_like(x)
+    err[..., a], err[..., b] = x[..., a] * cos + x[..., b] * sin, x[..., b] * cos + x[..., a] * sin
+    return 2.2 * U * err + 2.0 ** -48 * x.max(-1, keepdims=True)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("context,base", [(40, 1.0), (5000, 1e4), (1 << 24, 5e5), (524285 * 4096, 1e6)])
+def test_rotated_to_the_last_bits(context, base, interleaved):
+    """Angles up to 2^51 (frequencies up to 2^20), each pair to three half ulps of its parts."""
+    rng = np.random.default_rng([context % 1000, interleaved])
+    n, heads, dim, page = 24, 3, 128, 4096
+    max_pages = -(-context // page)
+    table = torch.full((1, max_pages), -1, dtype=torch.int32, device="cuda")
+    first = (context - n) // page
+    table[0, first:] = torch.arange(max_pages - first, device="cuda")
+    cache = q.new_kv_cache("f16", max_pages - first, page, 1, dim)
+    Q = rounded(rng.standard_normal((n, heads, dim)) * 2.0 ** rng.integers(-20, 20, (n, heads, 1)), "f32")
+    freq = (base ** (-2.0 * np.arange(dim // 2) / dim)).astype(np.float32)
+    freq[1::7] = rng.uniform(0.3, 7, freq[1::7].shape)
+    freq[2::7] = -rng.uniform(0.5, 1, freq[2::7].shape) * 2.0 ** rng.integers(0, 21, freq[2::7].shape)
+    freq[3::28] = 0
+    x = torch.from_numpy(Q).float().cuda()
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    out = torch.empty_like(x)
+    q.qtea_kv_append_rotated(cache, x, x[:, :1], x[:, 1:2], i32(0, n), i32(context), table, torch.from_numpy(freq).cuda(), out, interleaved=interleaved)
+    pos = np.arange(context - n, context)
+    check(out, None, ol.rotate(Q, pos, freq, interleaved), "f32", _turn_error(Q, pos, freq, interleaved))
