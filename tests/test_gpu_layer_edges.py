@@ -77,6 +77,96 @@ def test_gate_has_the_same_bits_at_any_alignment(x, out):
         assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("x,out", [("f16", "e4m3"), ("f32", "f32"), ("bf16", "f16")])
+def test_gate_of_many_rows(x, out):
+    """2^20 octs and more, two a thread: 517 x 2176 is 128 more than whole
+    workgroups take, so the last ones have threads with one oct and with none."""
+    rng = np.random.default_rng([len(x), len(out), 1])
+    rows, dim = 517, 17408
+    both = torch.from_numpy(3 * rng.standard_normal((rows, 2 * dim), np.float32)).to(TORCH[x]).cuda()
+    got, scale = room((rows + 1, dim), out)
+    q.qtea_silu_mul(both[:, :dim], both[:, dim:], got[:rows], out_scale=None if scale is None else scale[:rows])
+    assert (got[rows] == (7 if scale is None else 0x55)).all() and (scale is None or (scale[rows] == 0x55).all())
+    some = [0, 1, 120, 240, 241, 482, 515, 516]
+    gate, up = both[some, :dim].double().cpu().numpy(), both[some, dim:].double().cpu().numpy()
+    want = ol.silu_mul(gate, up)
+    check(got[some], None if scale is None else scale[some], want, out, _gate_error(gate, want, out))
+    # every row by one that was computed alone
+    alone, alone_scale = room((1, dim), out)
+    for r in range(0, rows, 37):
+        q.qtea_silu_mul(both[r:r + 1, :dim], both[r:r + 1, dim:], alone, out_scale=alone_scale)
+        assert torch.equal(alone[0], got[r]) and (scale is None or torch.equal(alone_scale[0], scale[r]))
+
+
+@pytest.mark.parametrize("rows,dim", [(1, 32), (3, 96), (70, 992)])
+def test_gate_of_unaligned_rows_into_8_bits(rows, dim):
+    rng = np.random.default_rng([rows, dim])
+    both = rounded(2 * rng.standard_normal((rows, 2 * dim + 1)), "f16")
+    d = torch.from_numpy(both).half().cuda()
+    got, scale = room((rows, dim), "e4m3")
+    q.qtea_silu_mul(d[:, 1:1 + dim], d[:, 1 + dim:], got, out_scale=scale)
+    gate, up = both[:, 1:1 + dim], both[:, 1 + dim:]
+    want = ol.silu_mul(gate, up)
+    check(got, scale, want, "e4m3", _gate_error(gate, want, "e4m3"))
+
+
+# -- the norm --------------------------------------------------------------------------
+def _norm_error(t, w, eps):
+    """As in tests/test_gpu_layer_rows.py: the addition, sums of up to 64 in a row, a
+    wave's 6 steps and its workgroup's 16 (half of them in the root), the factor's four
+    roundings and two products."""
+    return np.abs(ol.rms_norm(t, w, eps)[0]) * U * (1 + (64 + 6 + 16 + 2) / 2 + 4 + 2)
+
+
+@pytest.mark.parametrize("shift", [0, 1])
+@pytest.mark.parametrize("residual", [None, "f32", "bf16"])
+@pytest.mark.parametrize("out", ["e4m3", "f16"])
+@pytest.mark.parametrize("heads,dim", [(7, 96), (3, 128), (5, 512), (2, 1024), (2, 16416)])
+def test_norm_of_heads(heads, dim, out, residual, shift):
+    """Heads into 8 bits and with a residual, aligned and not: codes, scales and the
+    residual of each head at its own place, what lies between tokens as it was."""
+    rng = np.random.default_rng([heads, dim, len(out), shift])
+    tokens = 5
+    X = rounded(rng.standard_normal((tokens, heads, dim)) * 2.0 ** rng.integers(-5, 6, (tokens, heads, 1)), "bf16")
+    W = rounded(rng.uniform(0.5, 2, dim), "f32")
+    x = torch.zeros((tokens, heads * dim + 8 + shift), dtype=torch.bfloat16, device="cuda")
+    x[:, shift:shift + heads * dim] = torch.from_numpy(X).flatten(1).bfloat16()
+    R = r = wide_r = None
+    if residual:
+        R = rounded(rng.standard_normal(X.shape), residual)
+        wide_r = torch.full((tokens, (heads + 1) * dim), 7.0, dtype=TORCH[residual], device="cuda")
+        r = wide_r[:, :heads * dim].unflatten(1, (heads, dim))
+        r.copy_(torch.from_numpy(R))
+    got, scale = room((tokens, heads + 1, dim), out)
+    q.qtea_rms_norm(x[:, shift:shift + heads * dim].unflatten(1, (heads, dim)), torch.from_numpy(W).float().cuda(), got[:, :heads], residual=r, eps=1e-5,
+                    out_scale=None if scale is None else scale[:, :heads])
+    want, t = ol.rms_norm(X, W, 1e-5, R)
+    check(got[:, :heads], None if scale is None else scale[:, :heads], want, out, _norm_error(t, W, 1e-5))
+    assert (got[:, heads] == (7 if scale is None else 0x55)).all() and (scale is None or (scale[:, heads] == 0x55).all())
+    if residual:
+        assert torch.equal(r.cpu(), (torch.from_numpy(X).float() + torch.from_numpy(R).float()).to(TORCH[residual]))
+        assert (wide_r[:, heads * dim:] == 7).all()
+
+
+@pytest.mark.parametrize("rows,dim,x,out", [(8192, 5120, "bf16", "e4m3"), (16, 4096, "f32", "f16"), (3, 1001, "f16", "f32")])
+def test_norm_is_the_same_every_time(rows, dim, x, out):
+    """The same inputs give the same bits, alone or among other rows."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(rows)
+    X = torch.randn((rows, dim), generator=gen, device="cuda").to(TORCH[x])
+    R = torch.randn((rows, dim), generator=gen, device="cuda").to(TORCH[x])
+    results = []
+    for _ in range(3):
+        r, (got, scale) = R.clone(), room((rows, dim), out)
+        q.qtea_rms_norm(X, None, got, residual=r, eps=1e-5, out_scale=scale)
+        results.append((got, r, scale))
+    one, (got, scale) = R[-1:].clone(), room((1, dim), out)
+    q.qtea_rms_norm(X[-1:], None, got, residual=one, eps=1e-5, out_scale=scale)
+    for other in (*results[1:], None):
+        for a, b in zip(results[0], other or (got, one, scale)):
+            assert a is None and b is None or torch.equal(a if other else a[-1:], b)
+
+
 # -- sizes past 2^29 ---------------------------------------------------------------------
 def test_gate_of_a_row_past_2_to_the_29():
     dim = 2 ** 29 + 40
