@@ -71,7 +71,8 @@ enum { QTEA_E4M3 = 3 }; /* beside enum qtea_type */
  *   heads      1 .. 65535
  *   dim        1 .. QTEA_NORM_MAX_DIM
  * Operands are aligned to their elements; rows that are 16-byte aligned move
- * in wide accesses.  Sums are fp32: |t| up to about 1e18.
+ * in wide accesses.  Sums are fp32: the sum of squares has to stay below 2^128, as
+ * it does at any dim for |t| up to 2^55.
  * Errors: QTEA_ERR_INVALID_ARG, QTEA_ERR_HIP.
  */
 int qtea_rms_norm(const void* x, int x_type, int64_t x_stride, void* residual, int residual_type, int64_t residual_stride,

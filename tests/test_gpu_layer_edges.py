@@ -148,6 +148,32 @@ def test_norm_of_heads(heads, dim, out, residual, shift):
         assert (wide_r[:, heads * dim:] == 7).all()
 
 
+@pytest.mark.parametrize("dim", [96, 512, 8192, 16384, 65536])
+def test_norm_of_the_largest_and_smallest_values(dim):
+    """|t| up to 2^55, and rows whose squares are nothing beside eps."""
+    rng = np.random.default_rng(dim)
+    X = rounded(rng.choice([-1, 1], (4, dim)) * rng.uniform(0.5, 1, (4, dim)), "f32")
+    X *= 2.0 ** np.array([55, 40, -70, -100])[:, None]
+    x, out = torch.from_numpy(X).float().cuda(), torch.empty((4, dim), device="cuda")
+    q.qtea_rms_norm(x, None, out, eps=1e-30)
+    want, t = ol.rms_norm(X, None, float(np.float32(1e-30)))
+    check(out, None, want, "f32", _norm_error(t, None, 1e-30))
+
+
+@pytest.mark.parametrize("shift,pad", [(1, 0), (0, 3)])
+@pytest.mark.parametrize("heads,dim", [(1, 96), (5, 128), (3, 256), (1, 4096), (2, 5120), (1, 16384)])
+def test_norm_has_the_same_bits_at_any_alignment(heads, dim, shift, pad):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(dim)
+    X = torch.randn((9, heads * dim), generator=gen, device="cuda").half()
+    wide = torch.zeros((9, heads * dim + shift + pad), dtype=torch.float16, device="cuda")
+    wide[:, shift:shift + heads * dim] = X
+    a, b = torch.empty((9, heads, dim), device="cuda"), torch.empty((9, heads, dim), device="cuda")
+    q.qtea_rms_norm(X.unflatten(1, (heads, dim)), None, a, eps=1e-5)
+    q.qtea_rms_norm(wide[:, shift:shift + heads * dim].unflatten(1, (heads, dim)), None, b, eps=1e-5)
+    assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("rows,dim,x,out", [(8192, 5120, "bf16", "e4m3"), (16, 4096, "f32", "f16"), (3, 1001, "f16", "f32")])
 def test_norm_is_the_same_every_time(rows, dim, x, out):
     """The same inputs give the same bits, alone or among other rows."""
