@@ -56,6 +56,7 @@ __device__ __forceinline__ Block block_of(const PackArgs& a, int64_t b) {
   return {row >> 4, at >> 2, int((at & 3) * 16 + (row & 15))};
 }
 
+// Done once for a matrix: 128257 x 4096 of fp16 350 us (1.33 GB, 3.8 TB/s), back 390.
 template <int TYPE>
 __global__ __launch_bounds__(kThreads) void w4_pack_kernel(const PackArgs a) {
   for (int64_t b = int64_t(blockIdx.x) * kThreads + threadIdx.x; b < a.total; b += int64_t(gridDim.x) * kThreads) {
@@ -255,8 +256,11 @@ __device__ __forceinline__ uint32_t piece_to(int row, int lane) {
 // 16 rows of X, by way of LDS of its own (no barriers; a row's 64 pieces come in one
 // coalesced load, where the lanes' own pieces would touch 64 lines an instruction).
 // While a unit is multiplied, the next one is on its way.  Bound by start and end
-// of a launch at one row (4096 x 4096 3.6 us), by bringing the activations, as many
-// bytes as codes, at 16 (5120 x 17408 16.4 us, 2.9 TB/s).
+// of a launch at one row (4096 x 4096 3.6 us), by bringing the activations at 16: a
+// unit of them in 16 bits is 16 KB, of a strip's codes 4 (5120 x 17408, two strips
+// a group: 16.4 us, 2.9 TB/s of codes and twice that of activations).  ODD: 16-bit
+// loads, eight a piece, and all 16 rows whatever the batch (32000 x 5121 at 1, 16 and 40
+// rows 17.5, 84 and 215 us, 32000 x 5120 16.3, 17 and 24).
 template <int XT, int R, int ROWS, bool ODD>
 __global__ __launch_bounds__(kThreads) void w4_gemm_split_kernel(const GemmArgs a) {
   using T = Type<XT>;
@@ -364,9 +368,9 @@ __global__ __launch_bounds__(kThreads) void w4_gemm_split_kernel(const GemmArgs 
 // share their strips, each has a tile or two of every unit's four, and their
 // sums are added at the end: so a workgroup has four strips a wave to keep LDS
 // idle enough, and as few strips altogether as give every CU its share.  HBM bounds it
-// (128257 x 4096 at one row 45.5 us, 6.1 TB/s; a plain read of as many bytes 42), past 32
-// rows what a CU has to bring, decode and multiply (32000 x 5120 at 40 rows 24 us,
-// 17 at 16).  STREAM: codes are loaded as used once.
+// (128257 x 4096 at one row 45.5 us in a graph, 6.1 TB/s; a plain read of as many bytes
+// 42), past 32 rows what a CU has to bring, decode and multiply (32000 x 5120 at 40 rows
+// 24 us, 17 at 16).  STREAM: codes are loaded as used once.
 template <int XT, int CT, int PARTS, bool STREAM>
 __global__ __launch_bounds__(kThreads) void w4_gemm_wide_kernel(const GemmArgs a) {
   using T = Type<XT>;
